@@ -274,6 +274,145 @@ int buzz_set_policy(buzz_t ctx, int policy);
  * fp32 summation order. */
 int buzz_set_decode_cluster(buzz_t ctx, int cluster_size);
 
+/* ---- Rotation of queries and keys -------------------------------------------------------------
+ * What stands between a layer's projections and buzz_prefill / buzz_decode_step / buzz_paged_append:
+ * the RMS norm of every query and key head and its rotation by position, in one pass over both.
+ *   y = x / sqrt(mean(x^2) + eps) * weight                    (left out where the weight is NULL)
+ *   (a, b) -> (a cos - b sin, b cos + a sin),  angle = position * inv_freq[i],  i < rotary_dim / 2
+ * The pair of frequency i is (y[i], y[i + rotary_dim/2]), or (y[2i], y[2i + 1]) with `interleaved`;
+ * elements from rotary_dim on are normed and not rotated. Angles are formed and reduced in 64 bits,
+ * so that far positions keep their accuracy; all else is fp32, rounded once. */
+typedef struct buzz_rope_shape {
+  int32_t q_heads, kv_heads; /* heads of a token in q and in k                               */
+  int32_t head_dim;          /* d: 64 or 128                                                 */
+  int32_t rotary_dim;        /* a multiple of 16, 16..d                                      */
+  int32_t dtype;             /* BUZZ_F32 or BUZZ_BF16: q, k, weights and outputs             */
+  int32_t interleaved;       /* 0: halves are paired, 1: neighbours are                      */
+  float eps;                 /* added to the mean square, >= 0                               */
+  int32_t reserved;          /* 0                                                            */
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride; /* elements from one token to the next */
+} buzz_rope_shape;
+
+/* q [tokens][Hq][d] -> q_out, k [tokens][Hkv][d] -> k_out; a token's heads are contiguous, tokens are
+ * `*_stride` elements apart (a fused projection's output needs no copy). positions_dev int32 [tokens],
+ * inv_freq_dev fp32 [rotary_dim / 2], weights [d] of the element type or NULL. Each output may be its
+ * input (same pointer, same stride); no other overlap is allowed. tokens = 0 launches nothing.
+ * Rejects: head counts < 1; another head_dim, dtype or rotary_dim; eps < 0 or not finite; a stride that
+ * is less than heads * d or keeps rows from starting at a multiple of 16 bytes; tokens < 0; null or
+ * misaligned pointers. */
+int buzz_norm_rope(const buzz_rope_shape* shape, const void* q, const void* k, const int32_t* positions_dev,
+                   const float* inv_freq_dev, const void* q_weight, const void* k_weight, void* q_out,
+                   void* k_out, int tokens, void* stream);
+
+/* ---- Paged cache: layers that keep their whole history ----------------------------------------
+ * Beside the bounded caches above, a stack may hold layers whose history stays complete (the full
+ * cache the method is compared with; first layers that are left dense). Their keys and values live
+ * in pages of `page_tokens` tokens, given to sequences by the caller's page table, written and read
+ * here, and attended over by one new token per sequence.
+ *
+ * Buffers of a pool (owned by the caller), for layer l, page p, KV head h, slot s:
+ *   k, v              [layers][pages][Hkv][page_tokens][d]  elements of `cache_dtype`
+ *   k_scale, v_scale  [layers][pages][Hkv][page_tokens]     fp32, 8-bit caches only (else ignored)
+ *   bounds            [layers][pages][Hkv][2][d]            elements of `dtype`: the smallest and the
+ *                     largest value of each key dimension over the page's tokens, as they were given
+ *                     to buzz_paged_append; NULL where buzz_paged_select is not used
+ *   status            int32 [4]
+ * 8-bit rows: scale = max(amax / top, 2^-100), code = round(x / scale), ties to even, top = 448 for
+ * BUZZ_E4M3 and 127 for BUZZ_I8; both quotients are rounded to fp32. A row that holds an infinity or
+ * NaN reads back as NaN.
+ *
+ * Arguments that several calls share:
+ *   lens_dev  int32 [batch]: tokens of each sequence, those of the present append included
+ *   table_dev int32 [batch][table_stride]: physical page of each logical page of a sequence; entries
+ *             behind a sequence's last page are not read
+ *   max_len   an upper bound on lens (host value), at most table_stride * page_tokens
+ * The library never reads the device arrays on the host. On the device, a length outside [0, bound] or
+ * a page outside the pool records BUZZ_ERR_INVALID at buzz_paged_status(): such a sequence is skipped
+ * and its rows are left as they were; of a bad page the tokens are skipped and take no part.
+ * A sequence of length 0 attends to nothing: output 0, log-sum-exp -infinity. */
+enum { BUZZ_E4M3 = 2, BUZZ_I8 = 3 };
+
+typedef struct buzz_paged* buzz_paged_t;
+
+typedef struct buzz_paged_shape {
+  int32_t layers;
+  int32_t pages;             /* pages of the pool, per layer                                 */
+  int32_t page_tokens;       /* 16, 32, 64 or 128                                            */
+  int32_t q_heads, kv_heads; /* q_heads / kv_heads: 1, 2, 4 or 8                             */
+  int32_t head_dim;          /* 64 or 128                                                    */
+  int32_t dtype;             /* BUZZ_F32 or BUZZ_BF16: q, new rows, rows read back, outputs  */
+  int32_t cache_dtype;       /* the same, or BUZZ_E4M3 or BUZZ_I8                            */
+  int32_t flags;             /* BUZZ_FLAG_LOGN: logits scaled by log_512(length)/sqrt(d)     */
+} buzz_paged_shape;
+
+typedef struct buzz_paged_buffers {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  void* bounds;
+  int32_t* status;
+} buzz_paged_buffers;
+
+/* Creates the host object and zeroes the status words (one synchronous memset); the pool's contents
+ * are taken as they are. Rejects what the comments above do not allow, null or misaligned (16 bytes)
+ * buffers, and scales missing from an 8-bit cache. */
+int buzz_paged_create(buzz_paged_t* out, const buzz_paged_shape* shape, const buzz_paged_buffers* buffers);
+void buzz_paged_destroy(buzz_paged_t ctx);
+
+/* Writes new rows k, v [total_tokens][Hkv][d], packed over `batch` sequences by cu_seqlens_dev
+ * [batch+1] (NULL: one token per sequence, total_tokens = batch). The tokens of sequence b become its
+ * last ones, positions lens[b] - new .. lens[b] - 1. Where the pool has bounds, a page's bounds are
+ * widened, or begun where its first slot is written; a NaN does not count in them. `max_new` is an
+ * upper bound on the new tokens of a sequence. No page may be written through two sequences at once.
+ * Rejects: layer or batch out of range (batch 1..65535), total_tokens < 1, max_new < 1 or > total_tokens,
+ * table_stride < 1, null or misaligned pointers. */
+int buzz_paged_append(buzz_paged_t ctx, int layer, const void* k, const void* v, const int32_t* cu_seqlens_dev,
+                      int batch, int total_tokens, int max_new, const int32_t* lens_dev,
+                      const int32_t* table_dev, int table_stride, void* stream);
+
+/* The inverse: copies the last tokens of each sequence (counts from cu_seqlens_dev, as above) out of
+ * the pages to k_out, v_out [total_tokens][Hkv][d], scaled back and rounded to `dtype`. */
+int buzz_paged_read(buzz_paged_t ctx, int layer, void* k_out, void* v_out, const int32_t* cu_seqlens_dev,
+                    int batch, int total_tokens, int max_new, const int32_t* lens_dev,
+                    const int32_t* table_dev, int table_stride, void* stream);
+
+/* Workspace that one buzz_paged_decode and one buzz_paged_select call of this size need. It holds
+ * nothing between calls; calls that may run at the same time need one each. */
+int buzz_paged_workspace_bytes(buzz_paged_t ctx, int batch, int max_len, size_t* decode_bytes,
+                               size_t* select_bytes);
+
+/* Attention of one new token per sequence over its pages: q, out [batch][Hq][d], out = Softmax(q k^T /
+ * sqrt(d)) v over the lens[b] tokens; lse fp32 [batch][Hq] (or NULL) receives the natural logarithm
+ * of the sum of the exponentials of the logits, by which results over disjoint tokens can be joined.
+ * The new token's own row is attended to if it has been appended before.
+ * `selected` (or NULL: all pages) int32 [batch][Hkv][selected_stride] lists the logical pages to attend
+ * to, per KV head: the first min(pages of the sequence, selected_stride) entries, each page once, in
+ * any order; an entry outside the sequence's pages is treated as a bad page.
+ * Split over the length where there are few sequences, and joined in a fixed order: results do not
+ * depend on timing. */
+int buzz_paged_decode(buzz_paged_t ctx, int layer, const void* q, const int32_t* lens_dev,
+                      const int32_t* table_dev, int table_stride, int batch, int max_len,
+                      const int32_t* selected, int selected_stride, void* out, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Chooses the pages that a new token attends to, per sequence and KV head: the first `sink` pages, the
+ * last `recent`, and of those between the `top` with the largest
+ *   score(page) = sum over the group's queries of sum over d of max(q_d low_d, q_d high_d),
+ * an upper bound on the sum of the logits any of the page's keys can have; formed in 64 bits, ties to
+ * the lowest page, NaN above all. selected int32 [batch][Hkv][sink + recent + top] receives the logical
+ * pages in ascending order, then -1: just what buzz_paged_decode takes. A sequence with no more pages
+ * than that keeps them all. Needs bounds.
+ * Rejects: no bounds; sink < 0, recent < 1, top < 0, or a sum above 32768; else as buzz_paged_decode. */
+int buzz_paged_select(buzz_paged_t ctx, int layer, const void* q, const int32_t* lens_dev,
+                      const int32_t* table_dev, int table_stride, int batch, int max_len, int sink,
+                      int recent, int top, int32_t* selected, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* As buzz_status and buzz_launch_count, for a paged cache. */
+int buzz_paged_status(buzz_paged_t ctx, void* stream);
+int64_t buzz_paged_launch_count(buzz_paged_t ctx);
+
 /* Static description of an error code. */
 const char* buzz_error_string(int code);
 

@@ -15,9 +15,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libbuzz.so")
 _lib = None
 
-BUZZ_F32, BUZZ_BF16 = 0, 1
+BUZZ_F32, BUZZ_BF16, BUZZ_E4M3, BUZZ_I8 = 0, 1, 2, 3
 BUZZ_FLAG_LOGN = 1
 _DTYPES = {torch.float32: BUZZ_F32, torch.bfloat16: BUZZ_BF16}
+_CACHE_DTYPES = {**_DTYPES, torch.float8_e4m3fn: BUZZ_E4M3, torch.int8: BUZZ_I8}
 
 
 class BuzzError(RuntimeError):
@@ -32,13 +33,30 @@ class _Shape(ctypes.Structure):
                  "max_prompt_tokens", "flags")]
 
 
+class _RopeShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("q_heads", "kv_heads", "head_dim", "rotary_dim", "dtype", "interleaved")] + \
+               [("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")]
+
+
+class _PagedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("layers", "pages", "page_tokens", "q_heads", "kv_heads", "head_dim", "dtype", "cache_dtype", "flags")]
+
+
+class _PagedBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "bounds", "status")]
+
+
 def exported_symbols() -> list[str]:
     """Every entry point include/buzz.h declares."""
     return ["buzz_workspace_bytes", "buzz_create", "buzz_destroy", "buzz_prefill", "buzz_decode_step",
             "buzz_decode_step_host", "buzz_decode_layers", "buzz_decode_layers_host", "buzz_evict", "buzz_export_state", "buzz_import_state",
             "buzz_export_prefill_scores", "buzz_prefill_static", "buzz_selftest_wait_expiry",
             "buzz_status", "buzz_launch_count", "buzz_set_decode_cluster", "buzz_set_sampling", "buzz_set_fused_evict",
-            "buzz_set_policy", "buzz_error_string"]
+            "buzz_set_policy", "buzz_error_string", "buzz_norm_rope", "buzz_paged_create", "buzz_paged_destroy",
+            "buzz_paged_append", "buzz_paged_read", "buzz_paged_workspace_bytes", "buzz_paged_decode", "buzz_paged_select",
+            "buzz_paged_status", "buzz_paged_launch_count"]
 
 
 def load_library(build_if_missing: bool = True):
@@ -95,6 +113,26 @@ def load_library(build_if_missing: bool = True):
     lib.buzz_set_decode_cluster.argtypes = [vp, ci]
     lib.buzz_error_string.restype = ctypes.c_char_p
     lib.buzz_error_string.argtypes = [ci]
+    lib.buzz_norm_rope.restype = ci
+    lib.buzz_norm_rope.argtypes = [ctypes.POINTER(_RopeShape)] + [vp] * 8 + [ci, vp]
+    lib.buzz_paged_create.restype = ci
+    lib.buzz_paged_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(_PagedShape), ctypes.POINTER(_PagedBuffers)]
+    lib.buzz_paged_destroy.restype = None
+    lib.buzz_paged_destroy.argtypes = [vp]
+    lib.buzz_paged_append.restype = ci
+    lib.buzz_paged_append.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, vp, vp, ci, vp]
+    lib.buzz_paged_read.restype = ci
+    lib.buzz_paged_read.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, vp, vp, ci, vp]
+    lib.buzz_paged_workspace_bytes.restype = ci
+    lib.buzz_paged_workspace_bytes.argtypes = [vp, ci, ci, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.buzz_paged_decode.restype = ci
+    lib.buzz_paged_decode.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, vp, ci, vp, vp, vp, sz, vp]
+    lib.buzz_paged_select.restype = ci
+    lib.buzz_paged_select.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, vp, sz, vp]
+    lib.buzz_paged_status.restype = ci
+    lib.buzz_paged_status.argtypes = [vp, vp]
+    lib.buzz_paged_launch_count.restype = ctypes.c_int64
+    lib.buzz_paged_launch_count.argtypes = [vp]
     _lib = lib
     return lib
 
@@ -258,3 +296,210 @@ class Buzz:
         _check(self._lib.buzz_export_prefill_scores(self._h, kv_head, total_tokens, out.data_ptr()),
                "buzz_export_prefill_scores")
         return out
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _tensor(name, x, device, dtype, shape=None):
+    """A contiguous tensor of this device, type and shape (None: any extent)."""
+    _need(x.device == device, f"{name}: on {x.device}, not on {device}")
+    _need(x.dtype == dtype, f"{name}: {x.dtype}, not {dtype}")
+    _need(x.is_contiguous(), f"{name}: not contiguous")
+    if shape is not None:
+        _need(x.dim() == len(shape) and all(b is None or a == b for a, b in zip(x.shape, shape)),
+              f"{name}: shape {tuple(x.shape)}, not {tuple(shape)}")
+    return x.data_ptr()
+
+
+class _On:
+    """Makes `device` and the stream to launch on current for a call, and restores what was; a stream
+    given by the caller has to be one of that device."""
+
+    def __init__(self, device, stream):
+        if stream is None:
+            self.ptr = torch.cuda.current_stream(device).cuda_stream
+            self._guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+        else:
+            _need(stream.device == device, f"stream: of {stream.device}, not of {device}")
+            self.ptr = stream.cuda_stream
+            self._guard = torch.cuda.stream(stream)      # what the call allocates belongs to that stream
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+        return self.ptr
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def _cuda_device(device) -> torch.device:
+    device = torch.device(device)
+    _need(device.type == "cuda", f"a CUDA device is needed, not {device}; there is no CPU fallback")
+    return torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+
+
+def _token_stride(name, x, device, dtype, shape):
+    """Elements between the tokens of [tokens, heads, d], whose heads are contiguous."""
+    _need(x.device == device, f"{name}: on {x.device}, not on {device}")
+    _need(x.dtype == dtype, f"{name}: {x.dtype}, not {dtype}")
+    _need(tuple(x.shape) == tuple(shape), f"{name}: shape {tuple(x.shape)}, not {tuple(shape)}")
+    _need(x.stride(2) == 1 and (shape[1] == 1 or x.stride(1) == shape[2]), f"{name}: a token's heads are not contiguous")
+    return x.stride(0) if shape[0] > 1 else max(x.stride(0), shape[1] * shape[2])
+
+
+def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps=1e-6, interleaved=False, q_out=None, k_out=None,
+              stream=None):
+    """buzz_norm_rope: RMS norm of every head of q [T, Hq, d] and k [T, Hkv, d] (where its weight [d] is given) and
+    rotation by `positions` (int32 [T]) at `inv_freq` (fp32 [rotary_dim / 2]). q and k may be slices of one
+    projection's output. Returns (q_out, k_out), made here unless given; an output may be its input."""
+    _need(q.dim() == 3 and k.dim() == 3, "q and k: [tokens, heads, d]")
+    device, dtype = _cuda_device(q.device), q.dtype
+    _need(dtype in _DTYPES, f"q: {dtype} is not supported")
+    T, d = q.shape[0], q.shape[2]
+    kshape = (T, k.shape[1], d)
+    sh = _RopeShape(q.shape[1], k.shape[1], d, 2 * inv_freq.numel(), _DTYPES[dtype], int(bool(interleaved)), eps, 0,
+                    _token_stride("q", q, device, dtype, q.shape), _token_stride("k", k, device, dtype, kshape))
+    pos, freq = _tensor("positions", positions, device, torch.int32, (T,)), _tensor("inv_freq", inv_freq, device, torch.float32, (None,))
+    qw = None if q_weight is None else _tensor("q_weight", q_weight, device, dtype, (d,))
+    kw = None if k_weight is None else _tensor("k_weight", k_weight, device, dtype, (d,))
+    with _On(device, stream) as s:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=device)
+        if k_out is None:
+            k_out = torch.empty(kshape, dtype=dtype, device=device)
+        sh.q_out_stride, sh.k_out_stride = _token_stride("q_out", q_out, device, dtype, q.shape), _token_stride("k_out", k_out, device, dtype, kshape)
+        _check(load_library().buzz_norm_rope(ctypes.byref(sh), q.data_ptr(), k.data_ptr(), pos, freq, qw, kw, q_out.data_ptr(),
+                                             k_out.data_ptr(), T, s), "buzz_norm_rope")
+    return q_out, k_out
+
+
+class BuzzPaged:
+    """A paged cache (all layers of a model shape): rows in and out, attention over pages, choice of pages.
+
+    The pool's tensors are attributes (k, v, and where there are any k_scale, v_scale, bounds), made here or
+    taken from `buffers` (a dict of those names). Method names mirror the C entry points. `lens` is int32
+    [batch], `table` int32 [batch, pages of a sequence at most].
+    """
+
+    def __init__(self, *, layers, pages, page_tokens, q_heads, kv_heads, head_dim, dtype, cache_dtype=None, bounds=False, logn=False,
+                 buffers=None, device="cuda:0"):
+        self._h = None
+        self._lib = load_library()
+        if not torch.cuda.is_available():
+            raise RuntimeError("libbuzz needs a CUDA device; there is no CPU fallback")
+        self.device = _cuda_device(device)
+        self.dtype, self.cache_dtype = dtype, dtype if cache_dtype is None else cache_dtype
+        _need(dtype in _DTYPES, f"dtype: {dtype} is not supported")
+        _need(self.cache_dtype in _CACHE_DTYPES, f"cache_dtype: {self.cache_dtype} is not supported")
+        self.layers, self.pages, self.page_tokens = int(layers), int(pages), int(page_tokens)
+        self.q_heads, self.kv_heads, self.head_dim = int(q_heads), int(kv_heads), int(head_dim)
+        _need(min(self.layers, self.pages, self.page_tokens, self.q_heads, self.kv_heads, self.head_dim) > 0, "sizes have to be positive")
+        rows = (self.layers, self.pages, self.kv_heads, self.page_tokens)
+        want = {"k": (rows + (self.head_dim,), self.cache_dtype), "v": (rows + (self.head_dim,), self.cache_dtype)}
+        if self.cache_dtype not in _DTYPES:
+            want["k_scale"] = want["v_scale"] = (rows, torch.float32)
+        if bounds:
+            want["bounds"] = (rows[:3] + (2, self.head_dim), dtype)
+        given = dict(buffers) if buffers is not None else {}
+        _need(not set(given) - set(want), f"buffers: {sorted(set(given) - set(want))} are not of this pool")
+        self.k = self.v = self.k_scale = self.v_scale = self.bounds = None
+        with torch.cuda.device(self.device):
+            for name, (shape, dt) in want.items():
+                if buffers is None:
+                    given[name] = torch.zeros(shape, dtype=torch.int8 if dt not in _DTYPES else dt, device=self.device).view(dt)
+                _need(name in given, f"buffers: {name} is missing")
+                _tensor(name, given[name], self.device, dt, shape)
+                setattr(self, name, given[name])
+            self._status = torch.zeros(4, dtype=torch.int32, device=self.device)
+            shape = _PagedShape(self.layers, self.pages, self.page_tokens, self.q_heads, self.kv_heads, self.head_dim, _DTYPES[dtype],
+                                _CACHE_DTYPES[self.cache_dtype], BUZZ_FLAG_LOGN if logn else 0)
+            buf = _PagedBuffers(*[None if t is None else t.data_ptr()
+                                  for t in (self.k, self.v, self.k_scale, self.v_scale, self.bounds, self._status)])
+            h = ctypes.c_void_p()
+            _check(self._lib.buzz_paged_create(ctypes.byref(h), ctypes.byref(shape), ctypes.byref(buf)), "buzz_paged_create")
+        self._h = h
+
+    def close(self):
+        if self._h is not None:
+            self._lib.buzz_paged_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _sequences(self, lens, table):
+        batch = lens.shape[0]
+        return (batch, _tensor("lens", lens, self.device, torch.int32, (batch,)),
+                _tensor("table", table, self.device, torch.int32, (batch, None)), table.shape[1])
+
+    def _rows(self, where, call, layer, k, v, lens, table, cu_seqlens, max_new, stream):
+        batch, lp, tp, stride = self._sequences(lens, table)
+        shape = (None, self.kv_heads, self.head_dim)
+        kp, vp = _tensor("k", k, self.device, self.dtype, shape), _tensor("v", v, self.device, self.dtype, shape)
+        _need(k.shape == v.shape, f"v: shape {tuple(v.shape)}, not {tuple(k.shape)}")
+        cu = None
+        if cu_seqlens is None:
+            _need(k.shape[0] == batch, "without cu_seqlens there is one token per sequence")
+            max_new = 1
+        else:
+            cu = _tensor("cu_seqlens", cu_seqlens, self.device, torch.int32, (batch + 1,))
+            max_new = k.shape[0] if max_new is None else max_new
+        with _On(self.device, stream) as s:
+            _check(call(self._h, layer, kp, vp, cu, batch, k.shape[0], max_new, lp, tp, stride, s), where)
+
+    def append(self, layer, k, v, lens, table, cu_seqlens=None, max_new=None, stream=None):
+        """buzz_paged_append: k, v [tokens, Hkv, d] become the last tokens of their sequences; `lens` counts them."""
+        self._rows("buzz_paged_append", self._lib.buzz_paged_append, layer, k, v, lens, table, cu_seqlens, max_new, stream)
+
+    def read(self, layer, lens, table, k_out, v_out, cu_seqlens=None, max_new=None, stream=None):
+        """buzz_paged_read: the last tokens of every sequence, as they are kept, to k_out, v_out [tokens, Hkv, d]."""
+        self._rows("buzz_paged_read", self._lib.buzz_paged_read, layer, k_out, v_out, lens, table, cu_seqlens, max_new, stream)
+
+    def _scratch(self, batch, max_len):
+        """Bytes of a decode's and of a select's workspace. The workspaces themselves are made per call, by the framework's
+        allocator and for the call's stream, so that no two calls share one."""
+        decode, select = ctypes.c_size_t(), ctypes.c_size_t()
+        _check(self._lib.buzz_paged_workspace_bytes(self._h, batch, max_len, ctypes.byref(decode), ctypes.byref(select)),
+               "buzz_paged_workspace_bytes")
+        return decode.value, max(select.value, 16)
+
+    def decode(self, layer, q, lens, table, max_len, out, lse=None, selected=None, stream=None):
+        """buzz_paged_decode: attention of one token per sequence, q and out [batch, Hq, d], lse fp32 [batch, Hq] or None;
+        `selected` int32 [batch, Hkv, n] limits it to those logical pages."""
+        batch, lp, tp, stride = self._sequences(lens, table)
+        shape = (batch, self.q_heads, self.head_dim)
+        qp, op = _tensor("q", q, self.device, self.dtype, shape), _tensor("out", out, self.device, self.dtype, shape)
+        ep = None if lse is None else _tensor("lse", lse, self.device, torch.float32, shape[:2])
+        sp = None if selected is None else _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, None))
+        with _On(self.device, stream) as s:
+            n = self._scratch(batch, max_len)[0]
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            _check(self._lib.buzz_paged_decode(self._h, layer, qp, lp, tp, stride, batch, max_len, sp,
+                                               0 if selected is None else selected.shape[2], op, ep, ws.data_ptr(), n, s), "buzz_paged_decode")
+
+    def select(self, layer, q, lens, table, max_len, sink, recent, top, selected, stream=None):
+        """buzz_paged_select: the pages for `decode`, into `selected` int32 [batch, Hkv, sink + recent + top]."""
+        batch, lp, tp, stride = self._sequences(lens, table)
+        _need(self.bounds is not None, "the pool has no bounds")
+        qp = _tensor("q", q, self.device, self.dtype, (batch, self.q_heads, self.head_dim))
+        sp = _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, sink + recent + top))
+        with _On(self.device, stream) as s:
+            n = self._scratch(batch, max_len)[1]
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            _check(self._lib.buzz_paged_select(self._h, layer, qp, lp, tp, stride, batch, max_len, sink, recent, top, sp, ws.data_ptr(), n, s),
+                   "buzz_paged_select")
+
+    def status(self, stream=None) -> int:
+        with _On(self.device, stream) as s:
+            return self._lib.buzz_paged_status(self._h, s)
+
+    def launch_count(self) -> int:
+        return self._lib.buzz_paged_launch_count(self._h)

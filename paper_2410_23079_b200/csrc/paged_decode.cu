@@ -1,0 +1,589 @@
+// Attention of one new token per sequence over its pages: o = softmax(q K^T / sqrt(d)) V per query head,
+// one KV head's rows shared by up to eight query heads.
+//
+// The work is one pass over K and V, so HBM bounds it. All sequences' rows form one line of work in
+// units of kWarps tiles of 16 tokens (sequence, then KV head, then length), and a grid of one block per
+// SM cuts that line into equal stretches: however ragged the batch, every block reads the same amount. A
+// stretch may begin or end inside a (sequence, KV head); such parts are written as (max, sum, output)
+// to the workspace and joined by a second, small kernel in the order of the line.
+//
+// A block's warps take the tiles of a unit in turn and are independent until their (sequence, KV head)
+// ends. Each keeps a ring of tiles in shared memory, filled by 16-byte asynchronous copies of its own
+// (no block barrier, and the next (sequence, KV head)'s rows are under way while one is finished).
+// Rows behind a sequence's end are filled with zeros, so nothing that a page holds there is multiplied.
+//
+// Both products run on m16n8k16 with the long index on the 16-row side and the group's heads on the
+// 8-column side, as in the bounded cache's decode kernel:
+//   S^T[16 keys x 8 heads] = K . Q^T     a lane's 16-byte chunk of a key row feeds E/4 products (E
+//                                        elements per chunk) under one order of d that Q shares
+//   O^T[16 dims x 8 heads] += V^T . P^T  lane takes chunk g + 8j of key rows 2t, 2t+1, 2t+8, 2t+9
+// The bf16 operands hold 8-bit codes exactly; the row scales multiply the logits and the probabilities.
+// fp32 operands are cut into three bf16 parts (8 + 8 + 8 bits), and the six products of weight 2^-16 and
+// above are added; probabilities are cut into two parts for bf16 outputs (2^-17, far below the output's
+// rounding) and three for fp32 outputs. Logits, maxima, sums and outputs are fp32.
+#include "paged_internal.cuh"
+
+namespace {
+
+using namespace buzz_paged_dev;
+
+constexpr int kTile = 16;
+constexpr int kHeads = 8;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct DecodeArgs {
+  const void* q;
+  void* out;
+  float* lse;
+  const int32_t *lens, *table, *selected;
+  int table_stride, selected_stride, batch, max_len, group, logn;
+  float scale_log2;
+  int4* desc;      // [blocks]: (instance whose join this block begins, or -1; last block of it)
+  float* part;     // [blocks][2][group * (D + 2)]: outputs, maxima, sums
+};
+
+template <typename T, typename C, int D>
+struct Plan {
+  static constexpr int kWarps = (C::kSize == 4) ? 4 : 8;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kRow = D * C::kSize;            // bytes of a row
+  static constexpr int kChunks = kRow / 16;            // 16-byte chunks of a row
+  static constexpr int kE = 16 / C::kSize;             // elements of a chunk
+  static constexpr int kStage = 2 * kTile * kRow + (C::kScaled ? 2 * kTile * 4 : 0);
+  static constexpr int kFit = (192 * 1024) / (kStage * kWarps);
+  static constexpr int kStages = kFit > 6 ? 6 : kFit;
+  static constexpr int kQ = sizeof(T) == 4 ? 3 : 1;    // bf16 parts of a query, of a probability, of a cached value
+  static constexpr int kP = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int kC = C::kSize == 4 ? 3 : 1;
+  static_assert(kStages >= 2, "a ring holds two tiles at least");
+  static size_t smem(int group) {
+    return (size_t)kWarps * kStages * kStage + sizeof(float) * ((size_t)kWarps * group * D + 2 * kWarps * kHeads);
+  }
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// 16 bytes global -> shared, or zeros where `on` is false (nothing is read then)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Two fp32 numbers as kN pairs of bf16 whose sums they are (to 8 kN bits).
+template <int kN>
+__device__ __forceinline__ void split(float a, float b, uint32_t (&w)[kN]) {
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    w[i] = pack_bf16(a, b);
+    if (i + 1 < kN) { a -= bf16_lo(w[i]); b -= bf16_hi(w[i]); }
+  }
+}
+
+// A 16-byte chunk of the cache as kE / 2 words of two bf16 values each, kC parts.
+template <typename C, int kC, int kE>
+__device__ __forceinline__ void chunk_to_bf16(const uint4& u, uint32_t (&w)[kC][kE / 2]) {
+  const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+  if constexpr (C::kSize == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[0][i] = x[i];
+  } else if constexpr (C::kSize == 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float f[4];
+      codes_to_float<C>(x[i], f);
+      w[0][2 * i] = pack_bf16(f[0], f[1]);
+      w[0][2 * i + 1] = pack_bf16(f[2], f[3]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t s[kC];
+      split<kC>(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]), s);
+#pragma unroll
+      for (int c = 0; c < kC; ++c) w[c][i] = s[c];
+    }
+  }
+}
+
+// Chunk positions are permuted per row so that the lanes of a 128-byte shared-memory wavefront meet
+// different banks: for K those are two neighbouring rows' four chunks, for V two chunks of rows 0, 2, 4, 6.
+template <int kChunks>
+__device__ __forceinline__ int swizzle_k(int row) { return kChunks >= 8 ? (row & 1) << 2 : 0; }
+template <int kChunks>
+__device__ __forceinline__ int swizzle_v(int row) { return kChunks >= 8 ? ((row >> 1) & 3) << 1 : (row >> 1) & 3; }
+
+// A place on the line of work.
+struct Place {
+  int b, h, unit;       // sequence, KV head, unit within (b, h)
+  int len, tiles, units;
+  bool bad;
+};
+
+__device__ __forceinline__ int tiles_of(const DecodeArgs& a, const PagedView& w, int len) {
+  if (!a.selected) return (len + kTile - 1) / kTile;
+  const int pages = (len + (1 << w.page_log2) - 1) >> w.page_log2;
+  return min(pages, a.selected_stride) << (w.page_log2 - 4);
+}
+template <int kWarps>
+__device__ __forceinline__ void load_sequence(const DecodeArgs& a, const PagedView& w, Place& p) {
+  const int len = a.lens[p.b];
+  p.bad = len < 0 || len > a.max_len;
+  p.len = p.bad ? 0 : len;
+  p.tiles = tiles_of(a, w, p.len);
+  p.units = max(1, (p.tiles + kWarps - 1) / kWarps);
+}
+template <int kWarps>
+__device__ __forceinline__ void advance(const DecodeArgs& a, const PagedView& w, Place& p) {
+  if (++p.unit < p.units) return;
+  p.unit = 0;
+  if (++p.h < w.kv_heads) return;
+  p.h = 0;
+  if (++p.b < a.batch) load_sequence<kWarps>(a, w, p);
+}
+
+template <typename T, typename C, int D>
+__global__ void __launch_bounds__(Plan<T, C, D>::kThreads, 1)
+paged_decode_kernel(const PagedView w, const DecodeArgs a) {
+  using L = Plan<T, C, D>;
+  constexpr int kWarps = L::kWarps, kThreads = L::kThreads, kChunks = L::kChunks, kE = L::kE, kStages = L::kStages;
+  constexpr int kMK = kE / 4;                    // products per chunk of K
+  constexpr int kKL = kChunks / 4;               // chunks per lane and key row
+  constexpr int kVJ = kChunks >= 8 ? kChunks / 8 : 1;
+  constexpr int kVE = D / 8 / kVJ;               // elements per lane, value row and j
+  constexpr int kOut = D / 16;                   // products per tile of V
+
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ long long warp_sum[kWarps];
+  __shared__ int found[2];
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, g = lane / 4, t = lane & 3;
+  unsigned char* ring = smem + (size_t)warp * kStages * L::kStage;
+  float* obuf = reinterpret_cast<float*>(smem + (size_t)kWarps * kStages * L::kStage);   // [warps][group][D]
+  float* wm = obuf + kWarps * a.group * D;       // [warps][8] maxima, then sums
+  float* wl = wm + kWarps * kHeads;
+
+  // ---- the line of work, and this block's stretch of it ----------------------------------------
+  long long mine = 0;
+  const int per = (a.batch + kThreads - 1) / kThreads;
+  const int b_lo = min(tid * per, a.batch), b_hi = min(b_lo + per, a.batch);
+  for (int b = b_lo; b < b_hi; ++b) {
+    Place p;
+    p.b = b;
+    load_sequence<kWarps>(a, w, p);
+    mine += p.units;
+    if (p.bad && blockIdx.x == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, b, a.lens[b]);
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long o = __shfl_up_sync(0xffffffffu, incl, off);
+    if (lane >= off) incl += o;
+  }
+  if (lane == 31) warp_sum[warp] = incl;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    if (i < warp) before += warp_sum[i];
+    total += warp_sum[i];
+  }
+  const long long U = total * w.kv_heads;
+  const int n = (int)min((long long)gridDim.x, U);
+  if ((int)blockIdx.x >= n) {
+    if (tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    return;
+  }
+  const long long u_begin = blockIdx.x * U / n, u_end = (blockIdx.x + 1) * U / n;
+  {
+    long long ex = (before + incl - mine) * w.kv_heads;
+    if (u_begin >= ex && u_begin < ex + mine * w.kv_heads) {
+      Place p;
+      int b = b_lo;
+      for (;; ++b) {
+        p.b = b;
+        load_sequence<kWarps>(a, w, p);
+        const long long here = (long long)p.units * w.kv_heads;
+        if (u_begin < ex + here) break;
+        ex += here;
+      }
+      found[0] = b;
+      found[1] = (int)(u_begin - ex);
+    }
+  }
+  __syncthreads();
+  Place cur;
+  cur.b = found[0];
+  load_sequence<kWarps>(a, w, cur);
+  cur.h = found[1] / cur.units;
+  cur.unit = found[1] - cur.h * cur.units;
+
+  // ---- the ring: one tile per unit and warp ------------------------------------------------------
+  Place ahead = cur;
+  long long u_ahead = u_begin;
+  const uint32_t ring32 = (uint32_t)__cvta_generic_to_shared(ring);
+  uint32_t rows_left = 0;                        // valid rows of the tiles in the ring, five bits a stage
+  auto fetch = [&](int stage) {
+    int rows = 0;
+    if (u_ahead < u_end) {
+      const int tile = ahead.unit * kWarps + warp;
+      if (tile < ahead.tiles) {
+        const int sub = w.page_log2 - 4;         // log2 of the tiles of a page
+        int lp = tile >> sub;
+        if (a.selected) lp = a.selected[((int64_t)ahead.b * w.kv_heads + ahead.h) * a.selected_stride + lp];
+        const int pages = (ahead.len + (1 << w.page_log2) - 1) >> w.page_log2;
+        int page = -1;
+        if (lp >= 0 && lp < pages) page = a.table[(int64_t)ahead.b * a.table_stride + lp];
+        if (page < 0 || page >= w.pages) {
+          if (lane == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, ahead.b, lp);
+        } else {
+          const int slot = (tile & ((1 << sub) - 1)) * kTile;
+          rows = min(kTile, max(0, ahead.len - ((lp << w.page_log2) + slot)));
+          if (rows > 0) {
+            const size_t row0 = ((((size_t)page * w.kv_heads + ahead.h) << w.page_log2) + slot);
+            const char* ks = w.k + row0 * L::kRow;
+            const char* vs = w.v + row0 * L::kRow;
+            const uint32_t kd = ring32 + stage * L::kStage, vd = kd + kTile * L::kRow;
+#pragma unroll
+            for (int i = 0; i < kTile * kChunks / 32; ++i) {
+              const int x = i * 32 + lane, r = x / kChunks, c = x % kChunks;
+              copy16(kd + r * L::kRow + ((c ^ swizzle_k<kChunks>(r)) * 16), ks + x * 16, r < rows);
+            }
+#pragma unroll
+            for (int i = 0; i < kTile * kChunks / 32; ++i) {
+              const int x = i * 32 + lane, r = x / kChunks, c = x % kChunks;
+              copy16(vd + r * L::kRow + ((c ^ swizzle_v<kChunks>(r)) * 16), vs + x * 16, r < rows);
+            }
+            if constexpr (C::kScaled) {
+              if (lane < 8) {
+                const float* src = (lane < 4 ? w.k_scale : w.v_scale) + row0 + (lane & 3) * 4;
+                copy16(kd + 2 * kTile * L::kRow + lane * 16, src, true);     // whole tiles of scales exist; unused ones are masked
+              }
+            }
+          }
+        }
+      }
+      ++u_ahead;
+      if (u_ahead < u_end) advance<kWarps>(a, w, ahead);
+    }
+    copy_commit();
+    rows_left = (rows_left & ~(31u << (5 * stage))) | ((uint32_t)rows << (5 * stage));
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) fetch(s);
+
+  float oc[kOut][4], m[2], l[2];
+  uint32_t qf[L::kQ][kKL * kMK][2];
+  int stage = 0;
+  bool first_part = cur.unit == 0;               // the present (sequence, KV head) was begun by this block
+  bool begin = true;
+  for (long long u = u_begin; u < u_end; ++u) {
+    if (begin) {
+      begin = false;
+      m[0] = m[1] = -INFINITY;
+      l[0] = l[1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kOut; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) oc[i][e] = 0.f;
+      const T* qp = static_cast<const T*>(a.q) + (((size_t)cur.b * w.kv_heads + cur.h) * a.group + g) * D;
+#pragma unroll
+      for (int i = 0; i < kKL; ++i)
+#pragma unroll
+        for (int mm = 0; mm < kMK; ++mm)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float lo = 0.f, hi = 0.f;
+            if (g < a.group) {
+              const int at = (4 * i + t) * kE + 4 * mm + 2 * x;
+              lo = (float)qp[at];
+              hi = (float)qp[at + 1];
+            }
+            uint32_t s[L::kQ];
+            split<L::kQ>(lo, hi, s);
+#pragma unroll
+            for (int c = 0; c < L::kQ; ++c) qf[c][i * kMK + mm][x] = s[c];
+          }
+    }
+    copy_wait<kStages - 2>();
+    __syncwarp();
+    fetch(stage == 0 ? kStages - 1 : stage - 1);   // the stage that the round before this one has read
+    const int rows = (rows_left >> (5 * stage)) & 31;
+    if (rows > 0) {
+      const unsigned char* kt = ring + stage * L::kStage;
+      const unsigned char* vt = kt + kTile * L::kRow;
+      // S^T = K Q^T
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kKL; ++i) {
+        uint32_t lo[L::kC][kE / 2], hi[L::kC][kE / 2];
+        const int c = (4 * i + t) ^ swizzle_k<kChunks>(g);             // rows g and g + 8 have one parity
+        chunk_to_bf16<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + g * L::kRow + c * 16), lo);
+        chunk_to_bf16<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + (g + 8) * L::kRow + c * 16), hi);
+#pragma unroll
+        for (int mm = 0; mm < kMK; ++mm)
+#pragma unroll
+          for (int kc = L::kC - 1; kc >= 0; --kc)
+#pragma unroll
+            for (int qc = L::kQ - 1; qc >= 0; --qc) {
+              if (kc + qc > 2) continue;
+              const uint32_t fr[4] = {lo[kc][2 * mm], hi[kc][2 * mm], lo[kc][2 * mm + 1], hi[kc][2 * mm + 1]};
+              mma_bf16(s, fr, qf[qc][i * kMK + mm][0], qf[qc][i * kMK + mm][1]);
+            }
+      }
+      // s[0], s[1]: key g, heads 2t, 2t+1; s[2], s[3]: key g + 8
+      float scale = a.scale_log2, vs0 = 1.f, vs1 = 1.f, ks0 = 1.f, ks1 = 1.f;
+      if (a.logn) scale *= __logf((float)cur.len) * (1.0f / 6.2383246250395077f);
+      if constexpr (C::kScaled) {
+        const float* sc = reinterpret_cast<const float*>(vt + kTile * L::kRow);
+        ks0 = sc[g]; ks1 = sc[g + 8]; vs0 = sc[kTile + g]; vs1 = sc[kTile + g + 8];
+        if (g >= rows) vs0 = 0.f;
+        if (g + 8 >= rows) vs1 = 0.f;
+      }
+      float p[4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        p[e] = g < rows ? s[e] * ks0 * scale : -INFINITY;
+        p[2 + e] = g + 8 < rows ? s[2 + e] * ks1 * scale : -INFINITY;
+        float top = fmaxf(p[e], p[2 + e]);
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const float next = fmaxf(m[e], top);
+        const float base = next == -INFINITY ? 0.f : next;             // keys of logit -inf weigh nothing
+        const float f = exp2f(m[e] - base);
+        m[e] = next;
+        p[e] = exp2f(p[e] - base);
+        p[2 + e] = exp2f(p[2 + e] - base);
+        l[e] = l[e] * f + (p[e] + p[2 + e]);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) { oc[i][e] *= f; oc[i][2 + e] *= f; }
+      }
+      // P^T fragments: the probabilities (times the values' scales), transposed from keys x heads
+      uint32_t pa[L::kP], pb[L::kP], f0[L::kP], f1[L::kP];
+      split<L::kP>(p[0] * vs0, p[1] * vs0, pa);
+      split<L::kP>(p[2] * vs1, p[3] * vs1, pb);
+#pragma unroll
+      for (int c = 0; c < L::kP; ++c) { f0[c] = transpose8x8(pa[c]); f1[c] = transpose8x8(pb[c]); }
+      // O^T += V^T P^T
+      int done = 0;
+#pragma unroll
+      for (int j = 0; j < kVJ; ++j) {
+        uint32_t vw[4][L::kC][kVE / 2];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int r = 2 * t + (x & 1) + (x >> 1) * 8;
+          if constexpr (kChunks >= 8) {
+            const int c = (g + 8 * j) ^ swizzle_v<kChunks>(r);
+            chunk_to_bf16<C, L::kC, kE>(*reinterpret_cast<const uint4*>(vt + r * L::kRow + c * 16), vw[x]);
+          } else {                               // 64 dims of 8 bits: eight bytes of a chunk
+            const int c = (g >> 1) ^ swizzle_v<kChunks>(r);
+            const uint2 half = *reinterpret_cast<const uint2*>(vt + r * L::kRow + c * 16 + (g & 1) * 8);
+            float fa[4], fb[4];
+            codes_to_float<C>(half.x, fa);
+            codes_to_float<C>(half.y, fb);
+            vw[x][0][0] = pack_bf16(fa[0], fa[1]); vw[x][0][1] = pack_bf16(fa[2], fa[3]);
+            vw[x][0][2] = pack_bf16(fb[0], fb[1]); vw[x][0][3] = pack_bf16(fb[2], fb[3]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kVE / 2; ++i) {
+#pragma unroll
+          for (int vc = L::kC - 1; vc >= 0; --vc) {
+            const uint32_t fr[4] = {__byte_perm(vw[0][vc][i], vw[1][vc][i], 0x5410), __byte_perm(vw[0][vc][i], vw[1][vc][i], 0x7632),
+                                    __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x5410), __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x7632)};
+#pragma unroll
+            for (int pc = L::kP - 1; pc >= 0; --pc)
+              if (vc + pc <= 2) mma_bf16(oc[done], fr, f0[pc], f1[pc]);
+          }
+          ++done;
+        }
+      }
+    }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+
+    // ---- end of this (sequence, KV head), or of the block's stretch of it -----------------------
+    const bool complete = cur.unit + 1 == cur.units;
+    if (complete || u + 1 == u_end) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) l[e] += __shfl_xor_sync(0xffffffffu, l[e], off);
+      if (g == 0) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { wm[warp * kHeads + 2 * t + e] = m[e]; wl[warp * kHeads + 2 * t + e] = l[e]; }
+      }
+      __syncthreads();
+      float top[2], f[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top[e] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) top[e] = fmaxf(top[e], wm[i * kHeads + 2 * t + e]);
+        f[e] = m[e] == -INFINITY ? 0.f : exp2f(m[e] - top[e]);
+      }
+#pragma unroll
+      for (int i = 0; i < kOut; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (2 * t + e >= a.group) continue;
+          const int j = i / (kVE / 2), k = i % (kVE / 2);
+          const int dim = (kChunks >= 8 ? (g + 8 * j) * kE : g * kVE) + 2 * k;
+          *reinterpret_cast<float2*>(obuf + (warp * a.group + 2 * t + e) * D + dim) = make_float2(oc[i][e] * f[e], oc[i][2 + e] * f[e]);
+        }
+      __syncthreads();
+      const bool whole = complete && first_part;
+      const size_t head0 = ((size_t)cur.b * w.kv_heads + cur.h) * a.group;
+      float* part = a.part + ((size_t)blockIdx.x * 2 + (first_part ? 1 : 0)) * a.group * (D + 2);
+      for (int x = tid; x < a.group * D; x += kThreads) {
+        const int hd = x / D;
+        float big = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) big = fmaxf(big, wm[i * kHeads + hd]);
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+          const float mi = wm[i * kHeads + hd];
+          sum += mi == -INFINITY ? 0.f : wl[i * kHeads + hd] * exp2f(mi - big);
+          o += obuf[i * a.group * D + x];
+        }
+        if (whole) {
+          if (!cur.bad) {
+            static_cast<T*>(a.out)[head0 * D + x] = (T)(sum == 0.f ? 0.f : o / sum);
+            if (a.lse && x % D == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (big + log2f(sum)) * 0.69314718055994531f;
+          }
+        } else {
+          part[x] = o;
+          if (x % D == 0) { part[a.group * D + hd] = big; part[a.group * (D + 1) + hd] = sum; }
+        }
+      }
+      if (!complete && tid == 0) {
+        // the join of an instance is described where the instance begins
+        if (first_part) {
+          const long long end = u + (cur.units - cur.unit);                      // its first unit past the end
+          a.desc[blockIdx.x] = make_int4((int)(cur.b * (long long)w.kv_heads + cur.h), (int)((end * n - 1) / U), 0, 0);
+        } else {
+          a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        }
+      }
+      if (complete && u + 1 == u_end && tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+      __syncthreads();
+      begin = true;
+      first_part = true;
+    }
+    if (u + 1 < u_end) advance<kWarps>(a, w, cur);
+  }
+}
+
+// Joins the parts of the (sequence, KV head) that begins in block blockIdx.x and ends in a later one.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const DecodeArgs a, int kv_heads) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int c0 = blockIdx.x;
+  const int4 d = a.desc[c0];
+  if (d.x < 0) return;
+  const int slot = a.group * (D + 2);
+  for (int x = threadIdx.x; x < a.group * D; x += blockDim.x) {
+    const int hd = x / D;
+    float big = -INFINITY;
+    for (int c = c0; c <= d.y; ++c) big = fmaxf(big, a.part[((size_t)c * 2 + (c == c0)) * slot + a.group * D + hd]);
+    float sum = 0.f, o = 0.f;
+    for (int c = c0; c <= d.y; ++c) {
+      const float* p = a.part + ((size_t)c * 2 + (c == c0)) * slot;
+      const float mi = p[a.group * D + hd];
+      const float f = mi == -INFINITY ? 0.f : exp2f(mi - big);
+      sum += p[a.group * (D + 1) + hd] * f;
+      o += p[x] * f;
+    }
+    const size_t head0 = (size_t)d.x * a.group;
+    static_cast<T*>(a.out)[head0 * D + x] = (T)(sum == 0.f ? 0.f : o / sum);
+    if (a.lse && x % D == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (big + log2f(sum)) * 0.69314718055994531f;
+  }
+}
+
+int blocks_for(const buzz_paged* c, int batch, long long max_tiles, int warps) {
+  const long long units = (long long)batch * c->sh.kv_heads * ((max_tiles + warps - 1) / warps > 0 ? (max_tiles + warps - 1) / warps : 1);
+  return (int)(units < c->sm_count ? units : c->sm_count);
+}
+
+template <typename T, typename C, int D>
+cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) {
+  using L = Plan<T, C, D>;
+  long long tiles = ((long long)a.max_len + kTile - 1) / kTile;
+  if (a.selected) {
+    const long long most = (long long)a.selected_stride << (c->page_log2 - 4);
+    const long long round = ((tiles >> (c->page_log2 - 4)) + 1) << (c->page_log2 - 4);
+    tiles = most < round ? most : round;
+  }
+  const int n = blocks_for(c, a.batch, tiles, L::kWarps);
+  const size_t smem = L::smem(c->group);
+  static BuzzSmemOptIn opt_in;
+  if (cudaError_t e = opt_in.ensure(paged_decode_kernel<T, C, D>, smem); e != cudaSuccess) return e;
+  paged_decode_kernel<T, C, D><<<n, L::kThreads, smem, stream>>>(c->view(layer), a);
+  if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  c->launches += 1;
+  if (tiles <= L::kWarps) return cudaSuccess;      // one unit per (sequence, KV head): nothing is ever split
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n);
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D>, (const DecodeArgs)a, c->sh.kv_heads);
+  if (e == cudaSuccess) c->launches += 1;
+  return e;
+}
+
+template <typename T, typename C>
+cudaError_t launch_d(buzz_paged* c, int layer, const DecodeArgs& a, cudaStream_t s) {
+  return c->sh.head_dim == 128 ? launch<T, C, 128>(c, layer, a, s) : launch<T, C, 64>(c, layer, a, s);
+}
+
+}  // namespace
+
+// bytes of a decode call's workspace: a descriptor and two parts per block
+size_t buzz_paged_decode_workspace(const buzz_paged* c) {
+  return (size_t)c->sm_count * (sizeof(int4) + 2 * sizeof(float) * c->group * (c->sh.head_dim + 2));
+}
+
+extern "C" int buzz_paged_decode(buzz_paged_t c, int layer, const void* q, const int32_t* lens_dev, const int32_t* table_dev,
+                                 int table_stride, int batch, int max_len, const int32_t* selected, int selected_stride, void* out,
+                                 float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || layer < 0 || layer >= c->sh.layers || batch < 1 || batch > 65535 || table_stride < 1) return BUZZ_ERR_INVALID;
+  if (max_len < 0 || max_len > (int64_t)table_stride * c->sh.page_tokens) return BUZZ_ERR_INVALID;
+  if (!q || !lens_dev || !table_dev || !out || !workspace || (selected && selected_stride < 1)) return BUZZ_ERR_INVALID;
+  const uintptr_t wide = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace);
+  const uintptr_t words = reinterpret_cast<uintptr_t>(lens_dev) | reinterpret_cast<uintptr_t>(table_dev) |
+                          reinterpret_cast<uintptr_t>(selected) | reinterpret_cast<uintptr_t>(lse);
+  if ((wide & 15u) || (words & 3u) || workspace_bytes < buzz_paged_decode_workspace(c)) return BUZZ_ERR_INVALID;
+  DecodeArgs a;
+  a.q = q; a.out = out; a.lse = lse;
+  a.lens = lens_dev; a.table = table_dev; a.selected = selected;
+  a.table_stride = table_stride; a.selected_stride = selected_stride; a.batch = batch; a.max_len = max_len;
+  a.group = c->group;
+  a.logn = (c->sh.flags & BUZZ_FLAG_LOGN) ? 1 : 0;
+  a.scale_log2 = kLog2e / sqrtf((float)c->sh.head_dim);
+  a.desc = static_cast<int4*>(workspace);
+  a.part = reinterpret_cast<float*>(a.desc + c->sm_count);
+  (void)cudaGetLastError();
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaErrorInvalidValue;
+  const bool f32 = c->sh.dtype == BUZZ_F32;
+  switch (c->sh.cache_dtype) {
+    case BUZZ_F32: e = launch_d<float, CacheF32>(c, layer, a, s); break;
+    case BUZZ_BF16: e = launch_d<__nv_bfloat16, CacheBF16>(c, layer, a, s); break;
+    case BUZZ_E4M3: e = f32 ? launch_d<float, CacheE4M3>(c, layer, a, s) : launch_d<__nv_bfloat16, CacheE4M3>(c, layer, a, s); break;
+    case BUZZ_I8: e = f32 ? launch_d<float, CacheI8>(c, layer, a, s) : launch_d<__nv_bfloat16, CacheI8>(c, layer, a, s); break;
+  }
+  return e == cudaSuccess ? BUZZ_OK : BUZZ_ERR_CUDA;
+}

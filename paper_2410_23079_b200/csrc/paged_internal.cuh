@@ -1,0 +1,112 @@
+// Internal definitions of the paged cache: host object, device view, and the conversions between a
+// cache's element types and what the kernels compute with.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "buzz.h"
+#include "buzz_internal.cuh"
+
+// One layer of a pool as the kernels see it.
+struct PagedView {
+  char* k;
+  char* v;
+  float* k_scale;
+  float* v_scale;
+  char* bounds;        // null where the pool has none
+  int32_t* status;
+  int pages;           // pages of the pool
+  int kv_heads;
+  int page_log2;       // log2(page_tokens)
+};
+
+struct buzz_paged {
+  buzz_paged_shape sh;
+  buzz_paged_buffers buf;
+  int group;
+  int page_log2;
+  int sm_count;        // multiprocessors of the device that was current at buzz_paged_create
+  size_t esize, csize; // bytes per element of `dtype` and of the cache
+  long long launches;
+  PagedView view(int layer) const {
+    const size_t rows = (size_t)layer * sh.pages * sh.kv_heads * sh.page_tokens;
+    PagedView w;
+    w.k = static_cast<char*>(buf.k) + rows * sh.head_dim * csize;
+    w.v = static_cast<char*>(buf.v) + rows * sh.head_dim * csize;
+    w.k_scale = buf.k_scale ? buf.k_scale + rows : nullptr;
+    w.v_scale = buf.v_scale ? buf.v_scale + rows : nullptr;
+    w.bounds = buf.bounds ? static_cast<char*>(buf.bounds) + (size_t)layer * sh.pages * sh.kv_heads * 2 * sh.head_dim * esize : nullptr;
+    w.status = buf.status;
+    w.pages = sh.pages;
+    w.kv_heads = sh.kv_heads;
+    w.page_log2 = page_log2;
+    return w;
+  }
+};
+
+// Element types of a cache as template tags.
+struct CacheF32 { static constexpr int kSize = 4; static constexpr bool kScaled = false; };
+struct CacheBF16 { static constexpr int kSize = 2; static constexpr bool kScaled = false; };
+struct CacheE4M3 { static constexpr int kSize = 1; static constexpr bool kScaled = true; static constexpr float kTop = 448.f; };
+struct CacheI8 { static constexpr int kSize = 1; static constexpr bool kScaled = true; static constexpr float kTop = 127.f; };
+
+namespace buzz_paged_dev {
+
+// Two e4m3 codes (low byte first) as fp32; exact.
+__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t codes) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), __NV_E4M3);
+  return __half22float2(__half2(h));
+}
+
+// One signed byte of a word as fp32, exact: a byte offset by 128 under the exponent of 2^23.
+__device__ __forceinline__ float i8_to_float(uint32_t offset_word, int i) {
+  return __uint_as_float(__byte_perm(offset_word, 0x4B000000u, 0x7650 + i)) - 8388736.f;
+}
+
+// Four codes of a word as fp32.
+template <typename C>
+__device__ __forceinline__ void codes_to_float(uint32_t w, float (&f)[4]) {
+  if constexpr (C::kTop == 448.f) {
+    const float2 a = e4m3x2_to_float2(w), b = e4m3x2_to_float2(w >> 16);
+    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
+  } else {
+    const uint32_t o = w ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = i8_to_float(o, i);
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Eight consecutive elements of `T` as fp32, and back. The pointer is 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(ws[i]); x[2 * i + 1] = bf16_hi(ws[i]); }
+  } else {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+  } else {
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+}
+
+}  // namespace buzz_paged_dev

@@ -1,0 +1,609 @@
+"""The rotation and the paged cache on the GPU, through the binding, against plain 64-bit forms."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2410_23079_b200 import BuzzError, BuzzPaged, norm_rope
+from tests import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, E4M3, I8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.int8
+KINDS = [(BF16, BF16), (BF16, E4M3), (BF16, I8), (F32, F32), (F32, E4M3), (F32, I8)]
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def within(got, want, bound, what=""):
+    got, bound = got.double().cpu(), bound.double()
+    assert torch.equal(torch.isfinite(got), torch.isfinite(want)), what
+    fine = torch.isfinite(want)
+    assert torch.equal(got[~fine].nan_to_num(7.0), want[~fine].nan_to_num(7.0)), what
+    over = ((got - want).abs() - bound)[fine]
+    assert over.numel() == 0 or float(over.max()) <= 0.0, (what, float(over.max()), float((got - want)[fine].abs().max()))
+
+
+# ---- rotation ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,rotary", [(128, 128), (128, 48), (64, 64), (64, 16), (128, 96)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads", [(1, (8, 2)), (17, (7, 1)), (2500, (4, 4))])
+def test_norm_rope(cuda_device, dtype, d, rotary, interleaved, tokens, heads):
+    g = gen(tokens + d + rotary)
+    wide = torch.randn(tokens, sum(heads) + 1, d, generator=g).to(dtype)           # a projection's output with one more head
+    q, k = wide[:, :heads[0]], wide[:, heads[0]:sum(heads)]
+    pos = torch.randint(-5, 1 << 20, (tokens,), generator=g).to(torch.int32)
+    pos[0] = 0 if tokens == 1 else (1 << 31) - 1
+    freq = (500000.0 ** (-torch.arange(0, rotary, 2).double() / rotary)).float()
+    qw, kw = [(1 + torch.randn(d, generator=g) / 4).to(dtype) for _ in range(2)]
+    wd = wide.to(DEV)
+    for a, b in ((qw, kw), (None, kw), (None, None)):
+        on = lambda x: None if x is None else x.to(DEV)
+        qo, ko = norm_rope(wd[:, :heads[0]], wd[:, heads[0]:sum(heads)], pos.to(DEV), freq.to(DEV), on(a), on(b), eps=1e-5, interleaved=interleaved)
+        for got, x, w in ((qo, q, a), (ko, k, b)):
+            want, bound = ref.norm_rope(x, w, pos, freq, 1e-5, interleaved)
+            within(got, want, bound)
+    assert torch.equal(wd.cpu(), wide)
+
+
+def test_norm_rope_in_place_strided_outputs_and_streams(cuda_device):
+    g = gen(5)
+    wide = torch.randn(33, 13, 128, generator=g).to(BF16)
+    pos, freq = torch.arange(33, dtype=torch.int32), (1e4 ** (-torch.arange(0, 128, 2).double() / 128)).float()
+    w = torch.ones(128).to(BF16)
+    a = wide.to(DEV)
+    qo, ko = norm_rope(a[:, :8], a[:, 8:10], pos.to(DEV), freq.to(DEV), w.to(DEV), None)
+    b, p, f, ww = wide.to(DEV), pos.to(DEV), freq.to(DEV), w.to(DEV)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    r = norm_rope(b[:, :8], b[:, 8:10], p, f, ww, None, q_out=b[:, :8], k_out=b[:, 8:10], stream=side)
+    side.synchronize()
+    assert r[0].data_ptr() == b.data_ptr()
+    assert torch.equal(b[:, :8], qo) and torch.equal(b[:, 8:10], ko) and torch.equal(b[:, 10:].cpu(), wide[:, 10:])
+    empty = norm_rope(a[:0, :8], a[:0, 8:10], p[:0], f)
+    assert empty[0].shape == (0, 8, 128)
+
+
+def test_norm_rope_refusals(cuda_device):
+    q, p, f = torch.zeros(4, 2, 64, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV), torch.ones(16, device=DEV)
+    for call in (lambda: norm_rope(q, q, p.long(), f), lambda: norm_rope(q, q.bfloat16(), p, f), lambda: norm_rope(q, q, p[:3], f),
+                 lambda: norm_rope(q, q, p, f.double()), lambda: norm_rope(q, q[:3], p, f), lambda: norm_rope(q.half(), q.half(), p, f),
+                 lambda: norm_rope(q.transpose(0, 1), q, p, f), lambda: norm_rope(q, q, p, f, q_weight=f),
+                 lambda: norm_rope(q, q, p, f, q_out=q[:3]), lambda: norm_rope(q, q, p.cpu(), f)):
+        with pytest.raises(ValueError):
+            call()
+    for bad in (f[:4], torch.ones(40, device=DEV)):
+        with pytest.raises(BuzzError):
+            norm_rope(q, q, p, bad)
+    with pytest.raises(BuzzError):
+        norm_rope(q, q, p, f, eps=-1.0)
+
+
+# ---- pool helpers --------------------------------------------------------------------------------
+
+def poison(pool):
+    """Fills every part of a pool with what must never show."""
+    for n in ("k", "v", "k_scale", "v_scale", "bounds"):
+        t = getattr(pool, n)
+        if t is not None:
+            if t.dtype in (E4M3, I8):
+                t.view(torch.int8).fill_(0x7f)                                   # NaN in e4m3
+            else:
+                t.fill_(math.nan)
+
+
+def make(dtype, kind, lens, page, Hq, H, d, g, bounds=True, spare=3, logn=False):
+    counts = [-(-n // page) for n in lens]
+    pool = BuzzPaged(layers=2, pages=sum(counts) + spare, page_tokens=page, q_heads=Hq, kv_heads=H, head_dim=d, dtype=dtype, cache_dtype=kind,
+                     bounds=bounds, logn=logn, device=DEV)
+    poison(pool)
+    perm = torch.randperm(pool.pages, generator=g).to(torch.int32)
+    table = torch.full((len(lens), max(max(counts), 1) + 1), -1, dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(counts):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    return pool, table, perm[at:]
+
+
+def pack(rows, H, d):
+    return torch.cat(rows) if rows else torch.zeros(0, H, d)
+
+
+def cu_of(counts):
+    return torch.tensor([0] + list(torch.tensor(counts).cumsum(0)), dtype=torch.int32)
+
+
+def kept(x, kind):
+    codes, scale = ref.quantise(x, kind)
+    return codes if scale is None else codes * scale[..., None]
+
+
+def dev_lens(lens):
+    return torch.tensor(lens, dtype=torch.int32, device=DEV)
+
+
+# ---- rows in and out -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("d,page,H", [(128, 16, 2), (64, 32, 3), (64, 128, 1)])
+def test_append_and_read(cuda_device, dtype, kind, d, page, H):
+    g = gen(d + page)
+    final = [1, page, page + 1, 3 * page - 1, 40, 0, 2 * page + 7]
+    pool, table, unused = make(dtype, kind, final, page, H, H, d, g)
+    bits = lambda x: x.view(torch.int32 if x.dtype == F32 else torch.uint8).cpu().clone()          # NaN compares by its bits
+    before = {n: bits(getattr(pool, n)) for n in ("k", "v", "k_scale", "bounds") if getattr(pool, n) is not None}
+    rows = [(torch.randn(n, H, d, generator=g) * torch.exp(2 * torch.randn(n, H, 1, generator=g))).to(dtype) for n in final]
+    vals = [torch.randn(n, H, d, generator=g).to(dtype) for n in final]
+    rows[3][1, 0] = 0
+    rows[3][2, 0, 5] = -3e38
+    # in three calls: part of each prompt, the rest but one (now and then nothing), single tokens
+    at = [0] * len(final)
+    for cut in (lambda n: n // 2, lambda n: n - 1, lambda n: n):
+        upto = [max(a, cut(n)) for a, n in zip(at, final)]
+        new = [u - a for u, a in zip(upto, at)]
+        k = pack([r[a:u] for r, a, u in zip(rows, at, upto)], H, d).to(DEV)
+        v = pack([r[a:u] for r, a, u in zip(vals, at, upto)], H, d).to(DEV)
+        if k.shape[0]:
+            pool.append(1, k, v, dev_lens(upto), table.to(DEV), cu_of(new).to(DEV), max(new))
+        at = upto
+    assert pool.status() == 0
+    ko, vo = torch.full((sum(final), H, d), 9.0, dtype=dtype, device=DEV), torch.full((sum(final), H, d), 9.0, dtype=dtype, device=DEV)
+    pool.read(1, dev_lens(final), table.to(DEV), ko, vo, cu_of(final).to(DEV))
+    assert pool.status() == 0
+    for got, x in ((ko, rows), (vo, vals)):
+        assert torch.equal(got.cpu(), kept(pack(x, H, d), kind).to(dtype)), "rows read back"
+    for b, n in enumerate(final):
+        want = ref.page_bounds(rows[b], page)
+        for i in range(-(-n // page)):
+            assert torch.equal(pool.bounds[1, table[b, i]].double().cpu(), want[i]), (b, i)
+    # slots behind a sequence, pages of nobody and the other layer are as they were
+    for n, old in before.items():
+        new = bits(getattr(pool, n))
+        assert torch.equal(new[0], old[0]), n
+        assert torch.equal(new[1][unused.long()], old[1][unused.long()]), n
+        if n != "bounds":
+            for b, m in enumerate(final):
+                if m % page:
+                    p = int(table[b, m // page])
+                    assert torch.equal(new[1][p][:, m % page:], old[1][p][:, m % page:]), (n, b)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+def test_append_one_token_each_without_cu_seqlens(cuda_device, dtype, kind):
+    g = gen(1)
+    page, H, d, lens = 16, 5, 64, [1, 16, 17, 33]
+    pool, table, _ = make(dtype, kind, lens, page, H, H, d, g)
+    k, v = torch.randn(4, H, d, generator=g).to(dtype), torch.randn(4, H, d, generator=g).to(dtype)
+    pool.bounds.zero_()
+    pool.append(0, k.to(DEV), v.to(DEV), dev_lens(lens), table.to(DEV))
+    ko, vo = torch.empty_like(k, device=DEV), torch.empty_like(v, device=DEV)
+    pool.read(0, dev_lens(lens), table.to(DEV), ko, vo)
+    assert pool.status() == 0
+    assert torch.equal(ko.cpu(), kept(k, kind).to(dtype)) and torch.equal(vo.cpu(), kept(v, kind).to(dtype))
+    for b, n in enumerate(lens):                             # slot 0 begins a page's bounds, a later one widens them
+        got = pool.bounds[0, table[b, (n - 1) // page]].cpu()
+        x = k[b]
+        want = torch.stack([x, x], 1) if (n - 1) % page == 0 else torch.stack([x.clamp_max(0), x.clamp_min(0)], 1)
+        assert torch.equal(got.float(), want.float()), b
+
+
+@pytest.mark.parametrize("dtype,kind", [(BF16, E4M3), (F32, I8), (BF16, BF16)])
+def test_rows_with_infinities_and_nan(cuda_device, dtype, kind):
+    pool, table, _ = make(dtype, kind, [16], 16, 1, 1, 64, gen(2))
+    k = torch.randn(16, 1, 64, generator=gen(3)).to(dtype)
+    k[3, 0, 7], k[5, 0, 9], k[6, 0, 1] = math.inf, math.nan, -math.inf
+    pool.append(0, k.to(DEV), k.to(DEV), dev_lens([16]), table.to(DEV), cu_of([16]).to(DEV))
+    ko, vo = torch.empty_like(k, device=DEV), torch.empty_like(k, device=DEV)
+    pool.read(0, dev_lens([16]), table.to(DEV), ko, vo, cu_of([16]).to(DEV))
+    got = ko.cpu()
+    if kind == dtype:
+        assert torch.equal(got.nan_to_num(nan=1234.0), k.nan_to_num(nan=1234.0))
+    else:
+        for r in range(16):
+            assert bool(got[r].isnan().all()) == (r in (3, 5, 6)), r
+    assert torch.equal(pool.bounds[0, table[0, 0]].double().cpu(), ref.page_bounds(k, 16)[0])
+
+
+# ---- attention -----------------------------------------------------------------------------------
+
+def attend_case(dtype, kind, lens, page, Hq, H, d, seed, logn=False, max_len=None):
+    g = gen(seed)
+    pool, table, _ = make(dtype, kind, lens, page, Hq, H, d, g, logn=logn)
+    ks = [torch.randn(n, H, d, generator=g).to(dtype) * torch.where(torch.rand(n, H, 1, generator=g) < 0.05, 4.0, 1.0).to(dtype) for n in lens]
+    vs = [torch.randn(n, H, d, generator=g).to(dtype) for n in lens]
+    if sum(lens):
+        pool.append(1, pack(ks, H, d).to(DEV), pack(vs, H, d).to(DEV), dev_lens(lens), table.to(DEV), cu_of(lens).to(DEV), max(lens))
+    q = torch.randn(len(lens), Hq, d, generator=g).to(dtype)
+    out, lse = torch.full((len(lens), Hq, d), 77.0, dtype=dtype, device=DEV), torch.full((len(lens), Hq), 77.0, device=DEV)
+    pool.decode(1, q.to(DEV), dev_lens(lens), table.to(DEV), max(lens) if max_len is None else max_len, out, lse=lse)
+    assert pool.status() == 0
+    for b, n in enumerate(lens):
+        scale = d ** -0.5 * (math.log(max(n, 1)) / math.log(512) if logn else 1.0)
+        o, e, ob, eb = ref.attention(q[b], kept(ks[b], kind).transpose(0, 1), kept(vs[b], kind).transpose(0, 1), dtype, scale)
+        within(out[b], o, ob, ("out", b, n))
+        within(lse[b], e, eb, ("lse", b, n))
+    return pool, table, ks, vs, q, out
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,H,page", [(2, 2, 16), (8, 1, 32), (6, 3, 64), (8, 2, 128)])
+def test_decode_lengths(cuda_device, dtype, kind, d, Hq, H, page):
+    attend_case(dtype, kind, [1, 0, 15, 16, 17, 63, 64, 65, 127, 128, 129, 0, 300, 511, 1000], page, Hq, H, d, 7 * d + Hq + page)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("Hq,H,lens", [(1, 1, [9001]), (32, 8, [517]), (8, 8, [2049, 3, 4095]), (4, 2, [0]), (16, 2, [1])])
+def test_decode_split_over_the_length(cuda_device, dtype, kind, Hq, H, lens):
+    attend_case(dtype, kind, lens, 16, Hq, H, 128, 11 + Hq)
+
+
+def test_decode_more_sequences_than_threads(cuda_device):
+    lens = [(37 * i) % 150 for i in range(700)]
+    attend_case(BF16, I8, lens, 32, 2, 1, 64, 3)
+
+
+@pytest.mark.parametrize("dtype,kind", [(BF16, BF16), (F32, E4M3)])
+def test_decode_logn(cuda_device, dtype, kind):
+    attend_case(dtype, kind, [1, 2, 100, 512, 1500], 32, 4, 2, 128, 5, logn=True)
+
+
+def test_decode_is_reproducible_and_ignores_a_loose_bound(cuda_device):
+    pool, table, ks, vs, q, out = attend_case(BF16, BF16, [3000, 17, 1], 16, 8, 2, 128, 9)
+    for _ in range(5):
+        again = torch.empty_like(out)
+        pool.decode(1, q.to(DEV), dev_lens([3000, 17, 1]), table.to(DEV), 3000, again)
+        assert torch.equal(again, out)
+    pool.decode(1, q.to(DEV), dev_lens([3000, 17, 1]), table.to(DEV), table.shape[1] * 16, again)
+    assert torch.equal(again, out)
+
+
+def test_decode_logits_of_minus_infinity_and_extreme_scales(cuda_device):
+    """Keys whose logits overflow to -inf weigh nothing; a query against huge keys takes the largest alone."""
+    g = gen(21)
+    pool, table, _ = make(BF16, BF16, [40], 16, 1, 1, 64, g)
+    q = torch.ones(1, 1, 64, dtype=BF16)
+    k, v = torch.randn(40, 1, 64, generator=g).to(BF16), torch.randn(40, 1, 64, generator=g).to(BF16)
+    k[:16] = -3e38                                            # a whole tile, and more, of -inf
+    k[20] = -3e38
+    pool.append(0, k.to(DEV), v.to(DEV), dev_lens([40]), table.to(DEV), cu_of([40]).to(DEV))
+    out, lse = torch.empty(1, 1, 64, dtype=BF16, device=DEV), torch.empty(1, 1, device=DEV)
+    pool.decode(0, q.to(DEV), dev_lens([40]), table.to(DEV), 40, out, lse=lse)
+    keep = [i for i in range(16, 40) if i != 20]
+    o, e, ob, eb = ref.attention(q[0], k[keep].double().transpose(0, 1), v[keep].double().transpose(0, 1), BF16)
+    within(out[0], o, ob)
+    within(lse[0], e, eb)
+    pool.decode(0, q.to(DEV), dev_lens([16]), table.to(DEV), 16, out, lse=lse)       # nothing else: a row of nothing
+    assert torch.equal(out.cpu(), torch.zeros(1, 1, 64, dtype=BF16)) and float(lse) == -math.inf
+
+
+def test_decode_bad_lengths_and_pages(cuda_device):
+    g = gen(31)
+    lens = [100, 50, 70]
+    pool, table, ks, vs, q, out = attend_case(BF16, E4M3, lens, 16, 2, 1, 64, 31)
+    good = out.clone()
+    for bad in (-1, 101, 1 << 30):
+        out.fill_(5.0)
+        lse = torch.full((3, 2), 5.0, device=DEV)
+        pool.decode(1, q.to(DEV), dev_lens([100, bad, 70]), table.to(DEV), 100, out, lse=lse)
+        assert pool.status() == -1 and pool.status() == 0
+        assert torch.equal(out[[0, 2]], good[[0, 2]]) and bool((out[1] == 5.0).all()) and bool((lse[1] == 5.0).all())
+    for page in (-1, pool.pages, 1 << 30):
+        t = table.clone()
+        t[2, 1] = page                                        # tokens 16..31 of the last sequence take no part
+        pool.decode(1, q.to(DEV), dev_lens(lens), t.to(DEV), 100, out)
+        assert pool.status() == -1
+        assert torch.equal(out[:2], good[:2])
+        keep = [i for i in range(70) if not 16 <= i < 32]
+        o, _, ob, _ = ref.attention(q[2], kept(ks[2][keep], E4M3).transpose(0, 1), kept(vs[2][keep], E4M3).transpose(0, 1), BF16)
+        within(out[2], o, ob)
+
+
+def test_append_bad_arguments_on_the_device(cuda_device):
+    pool, table, _ = make(BF16, BF16, [40, 40], 16, 1, 1, 64, gen(41))
+    keep = pool.k.view(torch.int16).clone()
+    x = torch.ones(8, 1, 64, dtype=BF16, device=DEV)
+    t = table.to(DEV)
+    for lens, cu in (([3, 4], [0, 4, 8]), ([65, 1000], [0, 4, 8]), ([-1, 8], [0, 0, 8]), ([20, 20], [0, 9, 8]), ([20, 20], [0, 0, 9])):
+        pool.append(0, x, x, dev_lens(lens), t, torch.tensor(cu, dtype=torch.int32, device=DEV), 8)
+        assert pool.status() == -1, (lens, cu)
+    t2 = t.clone()
+    t2[0, 0], t2[1, 0] = -1, pool.pages
+    keep2 = pool.k.view(torch.int16).clone()
+    pool.append(0, x, x, dev_lens([4, 4]), t2, torch.tensor([0, 4, 8], dtype=torch.int32, device=DEV), 4)
+    assert pool.status() == -1
+    assert torch.equal(pool.k.view(torch.int16), keep2)
+    assert not torch.equal(keep, keep2)                       # the sound sequences of the calls above were written
+
+
+def test_offsets_beyond_32_bits(cuda_device):
+    """Pages whose rows lie beyond 2^31 elements and 2^32 bytes of the pool."""
+    H, page, d = 8, 128, 128
+    pool = BuzzPaged(layers=1, pages=20000, page_tokens=page, q_heads=8, kv_heads=H, head_dim=d, dtype=BF16, bounds=True, device=DEV)
+    g = gen(51)
+    lens = [300, 129]
+    table = torch.tensor([[19999, 3, 17001], [16500, 19998, -1]], dtype=torch.int32)
+    ks, vs = [[torch.randn(n, H, d, generator=g).to(BF16) for n in lens] for _ in range(2)]
+    pool.append(0, pack(ks, H, d).to(DEV), pack(vs, H, d).to(DEV), dev_lens(lens), table.to(DEV), cu_of(lens).to(DEV))
+    ko, vo = torch.empty(429, H, d, dtype=BF16, device=DEV), torch.empty(429, H, d, dtype=BF16, device=DEV)
+    pool.read(0, dev_lens(lens), table.to(DEV), ko, vo, cu_of(lens).to(DEV))
+    assert torch.equal(ko.cpu(), pack(ks, H, d)) and torch.equal(vo.cpu(), pack(vs, H, d))
+    q, out = torch.randn(2, 8, d, generator=g).to(BF16), torch.empty(2, 8, d, dtype=BF16, device=DEV)
+    pool.decode(0, q.to(DEV), dev_lens(lens), table.to(DEV), 384, out)
+    for b in range(2):
+        o, _, ob, _ = ref.attention(q[b], ks[b].double().transpose(0, 1), vs[b].double().transpose(0, 1), BF16)
+        within(out[b], o, ob)
+    sel = torch.empty(2, H, 2, dtype=torch.int32, device=DEV)
+    pool.select(0, q.to(DEV), dev_lens(lens), table.to(DEV), 384, 0, 1, 1, sel)
+    for b in range(2):
+        want = ref.choose(q[b], ref.page_bounds(ks[b], page), 0, 1, 1)
+        assert sel[b].tolist() == [w + [-1] * (2 - len(w)) for w in want]
+    assert pool.status() == 0
+
+
+# ---- choice of pages, and attention over them ----------------------------------------------------
+
+def select_case(dtype, kind, lens, page, Hq, H, d, sink, recent, top, seed, tie=False):
+    g = gen(seed)
+    pool, table, _ = make(dtype, kind, lens, page, Hq, H, d, g)
+    ks = [torch.randn(n, H, d, generator=g).to(dtype) for n in lens]
+    if tie:                                                   # few different pages: many equal scores
+        for x in ks:
+            for i in range(0, x.shape[0] - page + 1, page):
+                x[i:i + page] = x[:page] * (1 + (i // page) % 3)
+    vs = [torch.randn(n, H, d, generator=g).to(dtype) for n in lens]
+    pool.append(1, pack(ks, H, d).to(DEV), pack(vs, H, d).to(DEV), dev_lens(lens), table.to(DEV), cu_of(lens).to(DEV), max(lens))
+    q = torch.randn(len(lens), Hq, d, generator=g).to(dtype)
+    n = sink + recent + top
+    sel = torch.full((len(lens), H, n), 99, dtype=torch.int32, device=DEV)
+    out, lse = torch.empty(len(lens), Hq, d, dtype=dtype, device=DEV), torch.empty(len(lens), Hq, device=DEV)
+    pool.select(1, q.to(DEV), dev_lens(lens), table.to(DEV), max(lens), sink, recent, top, sel)
+    pool.decode(1, q.to(DEV), dev_lens(lens), table.to(DEV), max(lens), out, lse=lse, selected=sel)
+    assert pool.status() == 0
+    G = Hq // H
+    for b, m in enumerate(lens):
+        want = ref.choose(q[b], ref.page_bounds(ks[b], page), sink, recent, top)
+        assert sel[b].tolist() == [w + [-1] * (n - len(w)) for w in want], b
+        k, v = kept(ks[b], kind).transpose(0, 1), kept(vs[b], kind).transpose(0, 1)
+        for h in range(H):
+            rows = [i for p in want[h] for i in range(p * page, min(m, (p + 1) * page))]
+            o, e, ob, eb = ref.attention(q[b, h * G:(h + 1) * G], k[h:h + 1, rows], v[h:h + 1, rows], dtype)
+            within(out[b, h * G:(h + 1) * G], o, ob, (b, h))
+            within(lse[b, h * G:(h + 1) * G], e, eb, (b, h))
+
+
+@pytest.mark.parametrize("dtype,kind,d", [(BF16, BF16, 128), (BF16, E4M3, 64), (F32, F32, 64), (F32, I8, 128)])
+@pytest.mark.parametrize("Hq,H,page,sink,recent,top", [(2, 2, 16, 1, 2, 5), (8, 1, 32, 0, 1, 3), (8, 2, 16, 3, 1, 0), (3, 3, 64, 0, 3, 1)])
+def test_select_and_decode(cuda_device, dtype, kind, d, Hq, H, page, sink, recent, top):
+    select_case(dtype, kind, [1, 0, 16, 100, 401, 1000, 1025], page, Hq, H, d, sink, recent, top, d + Hq + page)
+
+
+@pytest.mark.parametrize("top", [1, 7, 200, 1500])
+def test_select_many_pages(cuda_device, top):
+    select_case(BF16, BF16, [40000, 12345], 16, 2, 1, 64, 2, 4, top, top)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_select_ties_go_to_the_lowest_page(cuda_device, dtype):
+    select_case(dtype, dtype, [1600, 800, 2000], 16, 2, 2, 64, 1, 1, 11, 13, tie=True)
+
+
+def test_select_special_scores(cuda_device):
+    """Zeros of both signs tie, infinities and NaN have their places."""
+    pool, table, _ = make(F32, F32, [160], 16, 1, 1, 64, gen(1))
+    b = torch.zeros(10, 1, 2, 64)
+    b[1, 0, :, 0] = -0.0
+    b[2, 0, :, 0], b[3, 0, :, 0], b[4, 0, :, 0] = -1.0, math.inf, -math.inf
+    b[6, 0, 0, 0], b[6, 0, 1, 1] = math.nan, math.nan
+    b[7, 0, :, 0] = 2.0
+    pool.bounds[0, table[0, :10].long()] = b.to(DEV)
+    q = torch.zeros(1, 1, 64)
+    q[0, 0, 0] = 1.0
+    b[3, 0, :, 1:] = 0.0
+    for top in range(0, 9):
+        sel = torch.empty(1, 1, top + 1, dtype=torch.int32, device=DEV)
+        pool.select(0, q.to(DEV), dev_lens([160]), table.to(DEV), 160, 0, 1, top, sel)
+        # NaN: 6 (a NaN bound); 3 and 4 (infinity times the zeros of the other sign's half is NaN as well)
+        order = [3, 4, 6, 7, 0, 1, 5, 8, 2]
+        assert sel[0, 0].tolist() == sorted(order[:top]) + [9], top
+
+
+def test_select_bad_lengths_and_pages(cuda_device):
+    g = gen(61)
+    lens = [320, 320]
+    pool, table, _ = make(BF16, BF16, lens, 16, 1, 1, 64, g)
+    k = torch.randn(640, 1, 64, generator=g).to(BF16).to(DEV)
+    pool.append(0, k, k, dev_lens(lens), table.to(DEV), cu_of(lens).to(DEV))
+    q = torch.randn(2, 1, 64, generator=g).to(BF16).to(DEV)
+    good = torch.empty(2, 1, 6, dtype=torch.int32, device=DEV)
+    pool.select(0, q, dev_lens(lens), table.to(DEV), 320, 1, 1, 4, good)
+    sel = torch.full_like(good, 55)
+    pool.select(0, q, dev_lens([321, 320]), table.to(DEV), 320, 1, 1, 4, sel)
+    assert pool.status() == -1
+    assert bool((sel[0] == 55).all()) and torch.equal(sel[1], good[1])
+    t = table.clone()
+    t[0, 7] = -5
+    pool.select(0, q, dev_lens(lens), t.to(DEV), 320, 1, 1, 18, torch.empty(2, 1, 20, dtype=torch.int32, device=DEV))
+    assert pool.status() == 0                                 # every page is kept: none is scored
+    sel18 = torch.empty(2, 1, 19, dtype=torch.int32, device=DEV)
+    pool.select(0, q, dev_lens(lens), t.to(DEV), 320, 1, 1, 17, sel18)
+    assert pool.status() == -1
+    assert sel18[0, 0].tolist() == [i for i in range(20) if i != 7]      # the bad page is below all others
+    # a choice that names pages outside its sequence: their tokens take no part
+    out = torch.empty(2, 1, 64, dtype=BF16, device=DEV)
+    want = torch.empty_like(out)
+    pool.decode(0, q, dev_lens(lens), table.to(DEV), 320, want, selected=torch.tensor([[[3, 5]], [[3, 5]]], dtype=torch.int32, device=DEV))
+    assert pool.status() == 0
+    pool.decode(0, q, dev_lens(lens), table.to(DEV), 320, out, selected=torch.tensor([[[3, 5]], [[20, -1]]], dtype=torch.int32, device=DEV))
+    assert pool.status() == -1
+    assert torch.equal(out[0], want[0]) and bool((out[1] == 0).all())
+
+
+# ---- arguments -----------------------------------------------------------------------------------
+
+def test_refusals(cuda_device):
+    pool, table, _ = make(BF16, E4M3, [40, 30], 16, 4, 2, 64, gen(71))
+    t, lens = table.to(DEV), dev_lens([40, 30])
+    q, out = torch.zeros(2, 4, 64, dtype=BF16, device=DEV), torch.zeros(2, 4, 64, dtype=BF16, device=DEV)
+    x = torch.zeros(2, 2, 64, dtype=BF16, device=DEV)
+    sel = torch.zeros(2, 2, 3, dtype=torch.int32, device=DEV)
+    for call in (lambda: pool.decode(0, q.float(), lens, t, 40, out), lambda: pool.decode(0, q[:1], lens, t, 40, out),
+                 lambda: pool.decode(0, q, lens.long(), t, 40, out), lambda: pool.decode(0, q, lens, t[:1], 40, out),
+                 lambda: pool.decode(0, q, lens, t.cpu(), 40, out), lambda: pool.decode(0, q, lens, t, 40, out.transpose(0, 1)),
+                 lambda: pool.decode(0, q, lens, t, 40, out, lse=out[..., 0]), lambda: pool.decode(0, q, lens, t, 40, out, selected=sel[:, :1]),
+                 lambda: pool.append(0, x, x[:1], lens, t), lambda: pool.append(0, x[:1], x[:1], lens, t),
+                 lambda: pool.append(0, x.float(), x.float(), lens, t), lambda: pool.append(0, x, x, lens, t, cu_seqlens=lens),
+                 lambda: pool.select(0, q, lens, t, 40, 1, 1, 2, sel), lambda: pool.select(0, q, lens, t, 40, 0, 1, 2, sel.float())):
+        with pytest.raises(ValueError):
+            call()
+    before = pool.launch_count()
+    for call in (lambda: pool.decode(2, q, lens, t, 40, out), lambda: pool.decode(-1, q, lens, t, 40, out), lambda: pool.decode(0, q, lens, t, -1, out),
+                 lambda: pool.decode(0, q, lens, t, 16 * t.shape[1] + 1, out), lambda: pool.append(9, x, x, lens, t),
+                 lambda: pool.append(0, x, x, lens, t, cu_seqlens=cu_of([1, 1]).to(DEV), max_new=3),
+                 lambda: pool.append(0, x, x, lens, t, cu_seqlens=cu_of([1, 1]).to(DEV), max_new=0),
+                 lambda: pool.select(0, q, lens, t, 40, 3, 0, 0, sel), lambda: pool.select(0, q, lens, t, 40, -1, 1, 3, sel),
+                 lambda: pool.select(0, q, lens, t, 40, 0, 4, -1, sel), lambda: pool.select(0, q, lens, t, 4000, 1, 1, 1, sel)):
+        with pytest.raises(BuzzError) as e:
+            call()
+        assert e.value.code == -1
+    n = ctypes.c_size_t()
+    lib, h = pool._lib, pool._h
+    assert lib.buzz_paged_workspace_bytes(h, 0, 1, ctypes.byref(n), ctypes.byref(n)) == -1
+    assert lib.buzz_paged_decode(h, 0, q.data_ptr(), lens.data_ptr(), t.data_ptr(), t.shape[1], 2, 40, None, 0, out.data_ptr(), None,
+                                 x.data_ptr(), 8, None) == -1                      # a workspace that is too small
+    assert lib.buzz_paged_select(h, 0, q.data_ptr(), lens.data_ptr(), t.data_ptr(), t.shape[1], 2, 40, 1, 1, 1, sel.data_ptr(),
+                                 x.data_ptr(), 8, None) == -1
+    assert pool.launch_count() == before
+    bare, table, _ = make(BF16, BF16, [40, 30], 16, 4, 2, 64, gen(72), bounds=False)
+    with pytest.raises(ValueError):
+        bare.select(0, q, lens, t, 40, 1, 1, 1, sel)
+    with pytest.raises(ValueError):
+        BuzzPaged(layers=1, pages=2, page_tokens=16, q_heads=2, kv_heads=2, head_dim=64, dtype=BF16, buffers={"k": bare.k}, device=DEV)
+    with pytest.raises(ValueError):
+        BuzzPaged(layers=1, pages=2, page_tokens=16, q_heads=2, kv_heads=2, head_dim=64, dtype=torch.float16, device=DEV)
+    with pytest.raises(BuzzError):
+        BuzzPaged(layers=1, pages=2, page_tokens=24, q_heads=2, kv_heads=2, head_dim=64, dtype=BF16, device=DEV)
+
+
+# ---- a run of them together ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+@pytest.mark.parametrize("captured", [False, True])
+def test_prompts_then_steps_of_one_layer(cuda_device, kind, captured):
+    """Projections -> norm_rope -> append -> (select ->) decode, ragged prompts and then single tokens, as a layer
+    of a model runs them; the steps also replayed from one captured graph, on a stream of its own."""
+    g = gen(81)
+    page, Hq, H, d, steps = 16, 8, 2, 128, 20
+    prompts = [70, 1, 133]
+    final = [n + steps for n in prompts]
+    pool, table, _ = make(BF16, kind, final, page, Hq, H, d, g)
+    t = table.to(DEV)
+    freq = (1e4 ** (-torch.arange(0, d, 2).double() / d)).float()
+    qw, kw = [(1 + torch.randn(d, generator=g) / 8).to(BF16) for _ in range(2)]
+    wide = [torch.randn(n, Hq + 2 * H, d, generator=g).to(BF16) for n in final]
+    fd, qwd, kwd = freq.to(DEV), qw.to(DEV), kw.to(DEV)
+    x = torch.cat([w[:n] for w, n in zip(wide, prompts)]).to(DEV)
+    pos = torch.cat([torch.arange(n) for n in prompts]).to(torch.int32).to(DEV)
+    _, k = norm_rope(x[:, :Hq], x[:, Hq:Hq + H], pos, fd, qwd, kwd)
+    pool.append(0, k, x[:, Hq + H:].contiguous(), dev_lens(prompts), t, cu_of(prompts).to(DEV), max(prompts))
+    lens = dev_lens(prompts)
+    x = torch.empty(3, Hq + 2 * H, d, dtype=BF16, device=DEV)
+    out, sparse = [torch.empty(3, Hq, d, dtype=BF16, device=DEV) for _ in range(2)]
+    sel = torch.empty(3, H, 6, dtype=torch.int32, device=DEV)
+    v = torch.empty(3, H, d, dtype=BF16, device=DEV)
+    q_rot = torch.empty(3, Hq, d, dtype=BF16, device=DEV)
+
+    def step():
+        lens.add_(1)
+        q, k = norm_rope(x[:, :Hq], x[:, Hq:Hq + H], lens - 1, fd, qwd, kwd, q_out=q_rot)
+        v.copy_(x[:, Hq + H:])
+        pool.append(0, k, v, lens, t)
+        pool.decode(0, q, lens, t, max(final), out)
+        pool.select(0, q, lens, t, max(final), 1, 2, 3, sel)
+        pool.decode(0, q, lens, t, max(final), sparse, selected=sel)
+
+    graph = None
+    ks = [ref.norm_rope(w[:, Hq:Hq + H], kw, torch.arange(w.shape[0]), freq, 1e-6, False)[0] for w in wide]
+    for i in range(steps):
+        x.copy_(torch.stack([w[n + i] for w, n in zip(wide, prompts)]))
+        if captured and i == 3:
+            torch.cuda.synchronize()
+            graph, keep = torch.cuda.CUDAGraph(), lens.clone()
+            with torch.cuda.graph(graph):
+                step()
+            assert torch.equal(lens, keep)
+        if graph is not None:
+            graph.replay()
+        else:
+            step()
+        if i in (0, 2, 3, 9, steps - 1):
+            torch.cuda.synchronize()
+            for b, n in enumerate(prompts):
+                m = n + i + 1
+                # the rows as the pool holds them: their own accuracy is tested above
+                ko, vo = torch.empty(m, H, d, dtype=BF16, device=DEV), torch.empty(m, H, d, dtype=BF16, device=DEV)
+                one = lambda z: z[b:b + 1].contiguous()
+                pool.read(0, one(lens), one(t), ko, vo, cu_of([m]).to(DEV))
+                kk, vv = ko.double().cpu(), vo.double().cpu()
+                if kind == BF16:
+                    assert float((kk - ks[b][:m]).abs().max()) < 0.05
+                else:                                          # rounding to 16 bits on the way out is not in the attention
+                    pages, slot = table[b, torch.arange(m) // page].long(), torch.arange(m) % page
+                    rows = lambda z, s: z[0].view(torch.int8).cpu()[pages, :, slot].view(E4M3).double() * s[0].cpu()[pages, :, slot].double()[..., None]
+                    kk, vv = rows(pool.k, pool.k_scale), rows(pool.v, pool.v_scale)
+                o, _, ob, _ = ref.attention(q_rot[b].cpu(), kk.transpose(0, 1), vv.transpose(0, 1), BF16)
+                within(out[b], o, ob, (i, b))
+                want = sel[b].tolist()
+                for h in range(H):
+                    at = [r for p in want[h] if p >= 0 for r in range(p * page, min(m, (p + 1) * page))]
+                    G = Hq // H
+                    o, _, ob, _ = ref.attention(q_rot[b, h * G:(h + 1) * G].cpu(), kk.transpose(0, 1)[h:h + 1, at], vv.transpose(0, 1)[h:h + 1, at], BF16)
+                    within(sparse[b, h * G:(h + 1) * G], o, ob, (i, b, h))
+    assert pool.status() == 0
+
+
+def test_two_streams_at_once(cuda_device):
+    """Two decodes of one pool in flight on two streams: neither sees the other's workspace."""
+    pool, table, ks, vs, q, out = attend_case(BF16, BF16, [20000], 16, 8, 1, 128, 91)
+    qd, lens, t = q.to(DEV), dev_lens([20000]), table.to(DEV)
+    q2 = torch.randn_like(qd)
+    want = torch.empty_like(out)
+    pool.decode(1, q2, lens, t, 20000, want)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty(20, *out.shape, dtype=BF16, device=DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, x, o in zip(streams, (qd, q2), outs):
+            pool.decode(1, x, lens, t, 20000, o[i], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(outs[0][i], out) and torch.equal(outs[1][i], want) for i in range(20))
+
+
+def test_paged_and_bounded_caches_side_by_side(cuda_device):
+    """While nothing has been evicted, a bounded cache and a paged one of the same layer give the same attention."""
+    from tests.harness import make_buzz
+    import workloads
+    w = workloads.scaled(workloads.get("C4"), layers=1, batch=2, q_heads=8, kv_heads=2, prompt_min=200, prompt_max=200, decode_steps=4, window=64, budget=512)
+    bz = make_buzz(w)
+    q, k, v, cu = workloads.prefill_inputs(w, 0, DEV)
+    bz.prefill(0, q, k, v, cu, 200, torch.empty_like(q))
+    pool, table, _ = make(BF16, BF16, [204, 204], 32, 8, 2, 128, gen(3))
+    t = table.to(DEV)
+    pool.append(0, k, v, dev_lens([200, 200]), t, cu, 200)
+    dq, dk, dv = workloads.decode_inputs(w, 0, DEV)
+    for i in range(4):
+        a, b = torch.empty_like(dq[i]), torch.empty_like(dq[i])
+        bz.decode_step(0, dq[i], dk[i], dv[i], a)
+        lens = dev_lens([201 + i] * 2)
+        pool.append(0, dk[i], dv[i], lens, t)
+        pool.decode(0, dq[i], lens, t, 204, b)
+        torch.testing.assert_close(a.float(), b.float(), atol=2e-2, rtol=1e-2)
+    assert bz.status() == 0 and pool.status() == 0
+    bz.close()
