@@ -303,38 +303,54 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _tensor(name, x, device, dtype, shape=None):
-    """A contiguous tensor of this device, type and shape (None: any extent)."""
+def _same(shape, want) -> bool:
+    return len(shape) == len(want) and all(b is None or a == b for a, b in zip(shape, want))
+
+
+def _tensor(name, x, device, dtype, shape):
+    """The address of a contiguous tensor of this device, type and shape (None: any extent). What is wrong is put into
+    words only once something is: the words would cost more than the checks."""
+    if x.device == device and x.dtype is dtype and x.is_contiguous() and (x.shape == shape or _same(x.shape, shape)):
+        return x.data_ptr()
     _need(x.device == device, f"{name}: on {x.device}, not on {device}")
-    _need(x.dtype == dtype, f"{name}: {x.dtype}, not {dtype}")
-    _need(x.is_contiguous(), f"{name}: not contiguous")
-    if shape is not None:
-        _need(x.dim() == len(shape) and all(b is None or a == b for a, b in zip(x.shape, shape)),
-              f"{name}: shape {tuple(x.shape)}, not {tuple(shape)}")
-    return x.data_ptr()
+    _need(x.dtype is dtype, f"{name}: {x.dtype}, not {dtype}")
+    _need(_same(x.shape, shape), f"{name}: shape {tuple(x.shape)}, not {tuple(shape)}")
+    raise ValueError(f"{name}: not contiguous")
+
+
+def _token_stride(name, x, device, dtype, tokens, heads, d):
+    """Elements between the tokens of [tokens, heads, d], whose heads are contiguous."""
+    s0, s1, s2 = x.stride()
+    if x.device == device and x.dtype is dtype and x.shape == (tokens, heads, d) and s2 == 1 and (s1 == d or heads == 1):
+        return s0 if tokens > 1 else max(s0, heads * d)
+    _need(x.device == device, f"{name}: on {x.device}, not on {device}")
+    _need(x.dtype is dtype, f"{name}: {x.dtype}, not {dtype}")
+    _need(x.shape == (tokens, heads, d), f"{name}: shape {tuple(x.shape)}, not {(tokens, heads, d)}")
+    raise ValueError(f"{name}: a token's heads are not contiguous")
 
 
 class _On:
-    """Makes `device` and the stream to launch on current for a call, and restores what was; a stream
-    given by the caller has to be one of that device."""
+    """Makes `device` current for a call that launches on `stream` (None: the device's current one), with what the
+    call allocates belonging to that stream, and restores what was. A given stream has to be one of that device."""
+    __slots__ = ("ptr", "guard")
 
     def __init__(self, device, stream):
         if stream is None:
-            self.ptr = torch.cuda.current_stream(device).cuda_stream
-            self._guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+            self.ptr = torch._C._cuda_getCurrentRawStream(device.index)
+            self.guard = torch.cuda.device(device) if torch._C._cuda_getDevice() != device.index else None
         else:
             _need(stream.device == device, f"stream: of {stream.device}, not of {device}")
             self.ptr = stream.cuda_stream
-            self._guard = torch.cuda.stream(stream)      # what the call allocates belongs to that stream
+            self.guard = torch.cuda.stream(stream)
 
     def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
+        if self.guard is not None:
+            self.guard.__enter__()
         return self.ptr
 
     def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
 
 
 def _cuda_device(device) -> torch.device:
@@ -343,38 +359,36 @@ def _cuda_device(device) -> torch.device:
     return torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
 
 
-def _token_stride(name, x, device, dtype, shape):
-    """Elements between the tokens of [tokens, heads, d], whose heads are contiguous."""
-    _need(x.device == device, f"{name}: on {x.device}, not on {device}")
-    _need(x.dtype == dtype, f"{name}: {x.dtype}, not {dtype}")
-    _need(tuple(x.shape) == tuple(shape), f"{name}: shape {tuple(x.shape)}, not {tuple(shape)}")
-    _need(x.stride(2) == 1 and (shape[1] == 1 or x.stride(1) == shape[2]), f"{name}: a token's heads are not contiguous")
-    return x.stride(0) if shape[0] > 1 else max(x.stride(0), shape[1] * shape[2])
-
-
 def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps=1e-6, interleaved=False, q_out=None, k_out=None,
               stream=None):
     """buzz_norm_rope: RMS norm of every head of q [T, Hq, d] and k [T, Hkv, d] (where its weight [d] is given) and
     rotation by `positions` (int32 [T]) at `inv_freq` (fp32 [rotary_dim / 2]). q and k may be slices of one
     projection's output. Returns (q_out, k_out), made here unless given; an output may be its input."""
+    device, dtype = q.device, q.dtype
     _need(q.dim() == 3 and k.dim() == 3, "q and k: [tokens, heads, d]")
-    device, dtype = _cuda_device(q.device), q.dtype
-    _need(dtype in _DTYPES, f"q: {dtype} is not supported")
-    T, d = q.shape[0], q.shape[2]
-    kshape = (T, k.shape[1], d)
-    sh = _RopeShape(q.shape[1], k.shape[1], d, 2 * inv_freq.numel(), _DTYPES[dtype], int(bool(interleaved)), eps, 0,
-                    _token_stride("q", q, device, dtype, q.shape), _token_stride("k", k, device, dtype, kshape))
+    if device.type != "cuda":
+        raise ValueError(f"q: on {device}; there is no CPU fallback")
+    if dtype not in _DTYPES:
+        raise ValueError(f"q: {dtype} is not supported")
+    T, Hq, d = q.shape
+    Hk = k.shape[1]
     pos, freq = _tensor("positions", positions, device, torch.int32, (T,)), _tensor("inv_freq", inv_freq, device, torch.float32, (None,))
     qw = None if q_weight is None else _tensor("q_weight", q_weight, device, dtype, (d,))
     kw = None if k_weight is None else _tensor("k_weight", k_weight, device, dtype, (d,))
+    qs, ks = _token_stride("q", q, device, dtype, T, Hq, d), _token_stride("k", k, device, dtype, T, Hk, d)
     with _On(device, stream) as s:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dtype, device=device)
+            q_out, qos = torch.empty((T, Hq, d), dtype=dtype, device=device), Hq * d
+        else:
+            qos = _token_stride("q_out", q_out, device, dtype, T, Hq, d)
         if k_out is None:
-            k_out = torch.empty(kshape, dtype=dtype, device=device)
-        sh.q_out_stride, sh.k_out_stride = _token_stride("q_out", q_out, device, dtype, q.shape), _token_stride("k_out", k_out, device, dtype, kshape)
-        _check(load_library().buzz_norm_rope(ctypes.byref(sh), q.data_ptr(), k.data_ptr(), pos, freq, qw, kw, q_out.data_ptr(),
-                                             k_out.data_ptr(), T, s), "buzz_norm_rope")
+            k_out, kos = torch.empty((T, Hk, d), dtype=dtype, device=device), Hk * d
+        else:
+            kos = _token_stride("k_out", k_out, device, dtype, T, Hk, d)
+        sh = _RopeShape(Hq, Hk, d, 2 * inv_freq.shape[0], _DTYPES[dtype], 1 if interleaved else 0, eps, 0, qs, ks, qos, kos)
+        rc = load_library().buzz_norm_rope(sh, q.data_ptr(), k.data_ptr(), pos, freq, qw, kw, q_out.data_ptr(), k_out.data_ptr(), T, s)
+    if rc:
+        raise BuzzError(rc, "buzz_norm_rope")
     return q_out, k_out
 
 
@@ -423,6 +437,7 @@ class BuzzPaged:
             h = ctypes.c_void_p()
             _check(self._lib.buzz_paged_create(ctypes.byref(h), ctypes.byref(shape), ctypes.byref(buf)), "buzz_paged_create")
         self._h = h
+        self._decode_bytes = self._scratch_bytes(1, 0)[0]
 
     def close(self):
         if self._h is not None:
@@ -436,15 +451,16 @@ class BuzzPaged:
             pass
 
     def _sequences(self, lens, table):
+        _need(lens.dim() == 1 and table.dim() == 2, "lens: [batch], table: [batch, pages]")
         batch = lens.shape[0]
         return (batch, _tensor("lens", lens, self.device, torch.int32, (batch,)),
-                _tensor("table", table, self.device, torch.int32, (batch, None)), table.shape[1])
+                _tensor("table", table, self.device, torch.int32, (batch, table.shape[1])), table.shape[1])
 
     def _rows(self, where, call, layer, k, v, lens, table, cu_seqlens, max_new, stream):
         batch, lp, tp, stride = self._sequences(lens, table)
-        shape = (None, self.kv_heads, self.head_dim)
+        _need(k.dim() == 3, "k and v: [tokens, kv heads, d]")
+        shape = (k.shape[0], self.kv_heads, self.head_dim)
         kp, vp = _tensor("k", k, self.device, self.dtype, shape), _tensor("v", v, self.device, self.dtype, shape)
-        _need(k.shape == v.shape, f"v: shape {tuple(v.shape)}, not {tuple(k.shape)}")
         cu = None
         if cu_seqlens is None:
             _need(k.shape[0] == batch, "without cu_seqlens there is one token per sequence")
@@ -463,13 +479,12 @@ class BuzzPaged:
         """buzz_paged_read: the last tokens of every sequence, as they are kept, to k_out, v_out [tokens, Hkv, d]."""
         self._rows("buzz_paged_read", self._lib.buzz_paged_read, layer, k_out, v_out, lens, table, cu_seqlens, max_new, stream)
 
-    def _scratch(self, batch, max_len):
-        """Bytes of a decode's and of a select's workspace. The workspaces themselves are made per call, by the framework's
-        allocator and for the call's stream, so that no two calls share one."""
+    def _scratch_bytes(self, batch, max_len):
+        """Bytes of a decode's workspace (the same for every call) and of a select's. The workspaces themselves are made
+        per call, by the framework's allocator and for the call's stream, so that no two calls share one."""
         decode, select = ctypes.c_size_t(), ctypes.c_size_t()
-        _check(self._lib.buzz_paged_workspace_bytes(self._h, batch, max_len, ctypes.byref(decode), ctypes.byref(select)),
-               "buzz_paged_workspace_bytes")
-        return decode.value, max(select.value, 16)
+        _check(self._lib.buzz_paged_workspace_bytes(self._h, batch, max_len, decode, select), "buzz_paged_workspace_bytes")
+        return decode.value, select.value
 
     def decode(self, layer, q, lens, table, max_len, out, lse=None, selected=None, stream=None):
         """buzz_paged_decode: attention of one token per sequence, q and out [batch, Hq, d], lse fp32 [batch, Hq] or None;
@@ -477,10 +492,10 @@ class BuzzPaged:
         batch, lp, tp, stride = self._sequences(lens, table)
         shape = (batch, self.q_heads, self.head_dim)
         qp, op = _tensor("q", q, self.device, self.dtype, shape), _tensor("out", out, self.device, self.dtype, shape)
-        ep = None if lse is None else _tensor("lse", lse, self.device, torch.float32, shape[:2])
+        ep = None if lse is None else _tensor("lse", lse, self.device, torch.float32, (batch, self.q_heads))
         sp = None if selected is None else _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, None))
         with _On(self.device, stream) as s:
-            n = self._scratch(batch, max_len)[0]
+            n = self._decode_bytes
             ws = torch.empty(n, dtype=torch.uint8, device=self.device)
             _check(self._lib.buzz_paged_decode(self._h, layer, qp, lp, tp, stride, batch, max_len, sp,
                                                0 if selected is None else selected.shape[2], op, ep, ws.data_ptr(), n, s), "buzz_paged_decode")
@@ -492,7 +507,7 @@ class BuzzPaged:
         qp = _tensor("q", q, self.device, self.dtype, (batch, self.q_heads, self.head_dim))
         sp = _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, sink + recent + top))
         with _On(self.device, stream) as s:
-            n = self._scratch(batch, max_len)[1]
+            n = max(16, self._scratch_bytes(batch, max_len)[1])
             ws = torch.empty(n, dtype=torch.uint8, device=self.device)
             _check(self._lib.buzz_paged_select(self._h, layer, qp, lp, tp, stride, batch, max_len, sink, recent, top, sp, ws.data_ptr(), n, s),
                    "buzz_paged_select")

@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(kWarps * 32)
 append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ v, const int32_t* cu, int total_tokens, int max_new,
               const int32_t* lens, const int32_t* table, int table_stride, int touched) {
   constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+  begin();
   const int item = blockIdx.x * kWarps + threadIdx.x / 32;
   const int b = blockIdx.y, j = item / w.kv_heads, h = item - j * w.kv_heads;
   if (j >= touched) return;
@@ -159,6 +160,7 @@ __global__ void __launch_bounds__(kWarps * 32)
 read_kernel(const PagedView w, T* __restrict__ k, T* __restrict__ v, const int32_t* cu, int total_tokens, int max_new,
             const int32_t* lens, const int32_t* table, int table_stride, int touched) {
   constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+  begin();
   const int item = blockIdx.x * kWarps + threadIdx.x / 32;
   const int b = blockIdx.y, j = item / w.kv_heads, h = item - j * w.kv_heads;
   if (j >= touched) return;
@@ -191,12 +193,10 @@ cudaError_t launch(buzz_paged* c, int layer, const Call& a, cudaStream_t s) {
   const dim3 grid((unsigned)((items + kWarps - 1) / kWarps), a.batch);
   const int most = a.max_new == 1 ? 1 : touched;
   if (a.write)
-    append_kernel<T, C, D><<<grid, kWarps * 32, 0, s>>>(c->view(layer), (const T*)a.k, (const T*)a.v, a.cu, a.total_tokens, a.max_new,
-                                                        a.lens, a.table, a.table_stride, most);
-  else
-    read_kernel<T, C, D><<<grid, kWarps * 32, 0, s>>>(c->view(layer), (T*)a.k, (T*)a.v, a.cu, a.total_tokens, a.max_new, a.lens,
-                                                      a.table, a.table_stride, most);
-  return cudaGetLastError();
+    return buzz_launch_chained(append_kernel<T, C, D>, grid, kWarps * 32, 0, s, c->view(layer), (const T*)a.k, (const T*)a.v, a.cu,
+                               a.total_tokens, a.max_new, a.lens, a.table, a.table_stride, most);
+  return buzz_launch_chained(read_kernel<T, C, D>, grid, kWarps * 32, 0, s, c->view(layer), (T*)a.k, (T*)a.v, a.cu, a.total_tokens,
+                             a.max_new, a.lens, a.table, a.table_stride, most);
 }
 
 template <typename T, typename C>

@@ -17,10 +17,15 @@
 //   S^T[16 keys x 8 heads] = K . Q^T     a lane's 16-byte chunk of a key row feeds E/4 products (E
 //                                        elements per chunk) under one order of d that Q shares
 //   O^T[16 dims x 8 heads] += V^T . P^T  lane takes chunk g + 8j of key rows 2t, 2t+1, 2t+8, 2t+9
-// The bf16 operands hold 8-bit codes exactly; the row scales multiply the logits and the probabilities.
-// fp32 operands are cut into three bf16 parts (8 + 8 + 8 bits), and the six products of weight 2^-16 and
-// above are added; probabilities are cut into two parts for bf16 outputs (2^-17, far below the output's
-// rounding) and three for fp32 outputs. Logits, maxima, sums and outputs are fp32.
+// Operands of the products, all summed in fp32:
+//   bf16 caches  bf16; a probability as two parts (2^-17, far below the output's rounding)
+//   fp32 caches  three bf16 parts of 8 bits each of queries, probabilities, keys and values; the six products
+//                of weight 2^-16 and above
+//   8-bit caches fp16, which holds the codes exactly and costs half the conversion that bf16 would. Queries
+//                are scaled by a power of two per head to a largest magnitude of 2^14..2^15 (bf16 queries
+//                stay exact down to 2^-28 of it; fp32 queries are two parts). The values' row scales go
+//                into the probabilities, relative to the largest scale met so far and times 2^14, in two
+//                parts; outputs are rescaled when that largest one grows, as they are for the maximum.
 #include "paged_internal.cuh"
 
 namespace {
@@ -44,20 +49,22 @@ struct DecodeArgs {
 
 template <typename T, typename C, int D>
 struct Plan {
-  static constexpr int kWarps = (C::kSize == 4) ? 4 : 8;
+  static constexpr bool kHalf = C::kScaled;            // fp16 operands
+  static constexpr int kWarps = C::kSize == 4 ? 4 : C::kSize == 2 ? 8 : 16;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kRow = D * C::kSize;            // bytes of a row
   static constexpr int kChunks = kRow / 16;            // 16-byte chunks of a row
   static constexpr int kE = 16 / C::kSize;             // elements of a chunk
   static constexpr int kStage = 2 * kTile * kRow + (C::kScaled ? 2 * kTile * 4 : 0);
-  static constexpr int kFit = (192 * 1024) / (kStage * kWarps);
+  static constexpr int kSlots = 4;                     // outputs that warps leave for the merge at a time
+  static constexpr int kFit = (204 * 1024) / (kStage * kWarps);
   static constexpr int kStages = kFit > 6 ? 6 : kFit;
-  static constexpr int kQ = sizeof(T) == 4 ? 3 : 1;    // bf16 parts of a query, of a probability, of a cached value
-  static constexpr int kP = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int kQ = sizeof(T) == 2 ? 1 : kHalf ? 2 : 3;    // parts of a query, of a probability, of a cached value
+  static constexpr int kP = kHalf || sizeof(T) == 2 ? 2 : 3;
   static constexpr int kC = C::kSize == 4 ? 3 : 1;
   static_assert(kStages >= 2, "a ring holds two tiles at least");
   static size_t smem(int group) {
-    return (size_t)kWarps * kStages * kStage + sizeof(float) * ((size_t)kWarps * group * D + 2 * kWarps * kHeads);
+    return (size_t)kWarps * kStages * kStage + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads);
   }
 };
 
@@ -66,6 +73,17 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <bool kHalf>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (kHalf) mma_f16(c, a, b0, b1);
+  else mma_bf16(c, a, b0, b1);
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
@@ -80,36 +98,55 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Two fp32 numbers as kN pairs of bf16 whose sums they are (to 8 kN bits).
-template <int kN>
+// Two fp32 numbers as kN pairs of bf16 (or fp16) whose sums they are, to 8 (or 11) bits a part.
+template <int kN, bool kHalf>
 __device__ __forceinline__ void split(float a, float b, uint32_t (&w)[kN]) {
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    w[i] = pack_bf16(a, b);
-    if (i + 1 < kN) { a -= bf16_lo(w[i]); b -= bf16_hi(w[i]); }
+    if constexpr (kHalf) {
+      const __half2 h = __floats2half2_rn(a, b);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      if (i + 1 < kN) { a -= __low2float(h); b -= __high2float(h); }
+    } else {
+      w[i] = pack_bf16(a, b);
+      if (i + 1 < kN) { a -= bf16_lo(w[i]); b -= bf16_hi(w[i]); }
+    }
   }
 }
 
-// A 16-byte chunk of the cache as kE / 2 words of two bf16 values each, kC parts.
+// Four 8-bit codes of a word as two pairs of fp16, exact. int8: a byte offset by 128 below the exponent of 2^10.
+template <typename C>
+__device__ __forceinline__ void codes_to_half(uint32_t x, uint32_t& lo, uint32_t& hi) {
+  if constexpr (C::kTop == 448.f) {
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffffu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x >> 16), __NV_E4M3);
+    lo = a.x | ((uint32_t)a.y << 16);
+    hi = b.x | ((uint32_t)b.y << 16);
+  } else {
+    const uint32_t o = x ^ 0x80808080u;
+    const uint32_t a = __byte_perm(o, 0x64646464u, 0x4140), b = __byte_perm(o, 0x64646464u, 0x4342);
+    const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));     // 1152
+    const __half2 ha = __hsub2(*reinterpret_cast<const __half2*>(&a), off), hb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+    lo = *reinterpret_cast<const uint32_t*>(&ha);
+    hi = *reinterpret_cast<const uint32_t*>(&hb);
+  }
+}
+
+// A 16-byte chunk of the cache as kE / 2 words of two operands each, kC parts.
 template <typename C, int kC, int kE>
-__device__ __forceinline__ void chunk_to_bf16(const uint4& u, uint32_t (&w)[kC][kE / 2]) {
+__device__ __forceinline__ void chunk_to_words(const uint4& u, uint32_t (&w)[kC][kE / 2]) {
   const uint32_t x[4] = {u.x, u.y, u.z, u.w};
   if constexpr (C::kSize == 2) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[0][i] = x[i];
   } else if constexpr (C::kSize == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float f[4];
-      codes_to_float<C>(x[i], f);
-      w[0][2 * i] = pack_bf16(f[0], f[1]);
-      w[0][2 * i + 1] = pack_bf16(f[2], f[3]);
-    }
+    for (int i = 0; i < 4; ++i) codes_to_half<C>(x[i], w[0][2 * i], w[0][2 * i + 1]);
   } else {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       uint32_t s[kC];
-      split<kC>(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]), s);
+      split<kC, false>(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]), s);
 #pragma unroll
       for (int c = 0; c < kC; ++c) w[c][i] = s[c];
     }
@@ -155,8 +192,11 @@ __device__ __forceinline__ void advance(const DecodeArgs& a, const PagedView& w,
 template <typename T, typename C, int D>
 __global__ void __launch_bounds__(Plan<T, C, D>::kThreads, 1)
 paged_decode_kernel(const PagedView w, const DecodeArgs a) {
+  begin();
   using L = Plan<T, C, D>;
   constexpr int kWarps = L::kWarps, kThreads = L::kThreads, kChunks = L::kChunks, kE = L::kE, kStages = L::kStages;
+  constexpr int kSlots = L::kSlots;
+  constexpr bool kHalf = L::kHalf;
   constexpr int kMK = kE / 4;                    // products per chunk of K
   constexpr int kKL = kChunks / 4;               // chunks per lane and key row
   constexpr int kVJ = kChunks >= 8 ? kChunks / 8 : 1;
@@ -168,8 +208,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
   __shared__ int found[2];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, g = lane / 4, t = lane & 3;
   unsigned char* ring = smem + (size_t)warp * kStages * L::kStage;
-  float* obuf = reinterpret_cast<float*>(smem + (size_t)kWarps * kStages * L::kStage);   // [warps][group][D]
-  float* wm = obuf + kWarps * a.group * D;       // [warps][8] maxima, then sums
+  float* obuf = reinterpret_cast<float*>(smem + (size_t)kWarps * kStages * L::kStage);   // [slots][group][D]
+  float* wm = obuf + kSlots * a.group * D;       // [warps][8] maxima, then sums
   float* wl = wm + kWarps * kHeads;
 
   // ---- the line of work, and this block's stretch of it ----------------------------------------
@@ -282,6 +322,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
   for (int s = 0; s < kStages - 1; ++s) fetch(s);
 
   float oc[kOut][4], m[2], l[2];
+  float q_unit[2] = {1.f, 1.f}, v_ref = 0.f, v_unit = 0.f;   // 8-bit caches: 2^-e of a head's query, largest value scale, 2^14 over it
+
   uint32_t qf[L::kQ][kKL * kMK][2];
   int stage = 0;
   bool first_part = cur.unit == 0;               // the present (sequence, KV head) was begun by this block
@@ -295,24 +337,39 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
       for (int i = 0; i < kOut; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) oc[i][e] = 0.f;
+      v_ref = v_unit = 0.f;
       const T* qp = static_cast<const T*>(a.q) + (((size_t)cur.b * w.kv_heads + cur.h) * a.group + g) * D;
+      float qv[kKL * kMK][4];
+      float big = 0.f;
 #pragma unroll
       for (int i = 0; i < kKL; ++i)
 #pragma unroll
         for (int mm = 0; mm < kMK; ++mm)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            float lo = 0.f, hi = 0.f;
-            if (g < a.group) {
-              const int at = (4 * i + t) * kE + 4 * mm + 2 * x;
-              lo = (float)qp[at];
-              hi = (float)qp[at + 1];
-            }
-            uint32_t s[L::kQ];
-            split<L::kQ>(lo, hi, s);
-#pragma unroll
-            for (int c = 0; c < L::kQ; ++c) qf[c][i * kMK + mm][x] = s[c];
+          for (int x = 0; x < 4; ++x) {
+            float& y = qv[i * kMK + mm][x];
+            y = g < a.group ? (float)qp[(4 * i + t) * kE + 4 * mm + x] : 0.f;
+            big = fmaxf(big, fabsf(y));
           }
+      float unit = 1.f;
+      if constexpr (kHalf) {
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const int e = max((int)(__float_as_uint(big) >> 23), 15);           // 2^(e - 127) <= big
+        unit = __uint_as_float((uint32_t)(268 - e) << 23);                   // 2^(14 - (e - 127))
+        const float back = __uint_as_float((uint32_t)(e - 14) << 23);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) q_unit[x] = __shfl_sync(0xffffffffu, back, (2 * t + x) * 4);
+      }
+#pragma unroll
+      for (int i = 0; i < kKL * kMK; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint32_t s[L::kQ];
+          split<L::kQ, kHalf>(qv[i][2 * x] * unit, qv[i][2 * x + 1] * unit, s);
+#pragma unroll
+          for (int c = 0; c < L::kQ; ++c) qf[c][i][x] = s[c];
+        }
     }
     copy_wait<kStages - 2>();
     __syncwarp();
@@ -327,8 +384,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
       for (int i = 0; i < kKL; ++i) {
         uint32_t lo[L::kC][kE / 2], hi[L::kC][kE / 2];
         const int c = (4 * i + t) ^ swizzle_k<kChunks>(g);             // rows g and g + 8 have one parity
-        chunk_to_bf16<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + g * L::kRow + c * 16), lo);
-        chunk_to_bf16<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + (g + 8) * L::kRow + c * 16), hi);
+        chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + g * L::kRow + c * 16), lo);
+        chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + (g + 8) * L::kRow + c * 16), hi);
 #pragma unroll
         for (int mm = 0; mm < kMK; ++mm)
 #pragma unroll
@@ -337,74 +394,103 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
             for (int qc = L::kQ - 1; qc >= 0; --qc) {
               if (kc + qc > 2) continue;
               const uint32_t fr[4] = {lo[kc][2 * mm], hi[kc][2 * mm], lo[kc][2 * mm + 1], hi[kc][2 * mm + 1]};
-              mma_bf16(s, fr, qf[qc][i * kMK + mm][0], qf[qc][i * kMK + mm][1]);
+              mma<kHalf>(s, fr, qf[qc][i * kMK + mm][0], qf[qc][i * kMK + mm][1]);
             }
       }
       // s[0], s[1]: key g, heads 2t, 2t+1; s[2], s[3]: key g + 8
-      float scale = a.scale_log2, vs0 = 1.f, vs1 = 1.f, ks0 = 1.f, ks1 = 1.f;
+      float scale = a.scale_log2, vs0 = 1.f, vs1 = 1.f, ks0 = 1.f, ks1 = 1.f, grow = 1.f;
       if (a.logn) scale *= __logf((float)cur.len) * (1.0f / 6.2383246250395077f);
       if constexpr (C::kScaled) {
         const float* sc = reinterpret_cast<const float*>(vt + kTile * L::kRow);
         ks0 = sc[g]; ks1 = sc[g + 8]; vs0 = sc[kTile + g]; vs1 = sc[kTile + g + 8];
         if (g >= rows) vs0 = 0.f;
         if (g + 8 >= rows) vs1 = 0.f;
+        float big = fmaxf(vs0, vs1);
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
+        if (big > v_ref) {                                             // the same in all lanes
+          grow = v_ref / big;
+          v_ref = big;
+          v_unit = 16384.f / big;
+        }
+        vs0 *= v_unit;
+        vs1 *= v_unit;
       }
-      float p[4];
+      float p[4], f[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        p[e] = g < rows ? s[e] * ks0 * scale : -INFINITY;
-        p[2 + e] = g + 8 < rows ? s[2 + e] * ks1 * scale : -INFINITY;
+        p[e] = g < rows ? s[e] * (ks0 * (scale * q_unit[e])) : -INFINITY;
+        p[2 + e] = g + 8 < rows ? s[2 + e] * (ks1 * (scale * q_unit[e])) : -INFINITY;
         float top = fmaxf(p[e], p[2 + e]);
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
         const float next = fmaxf(m[e], top);
         const float base = next == -INFINITY ? 0.f : next;             // keys of logit -inf weigh nothing
-        const float f = exp2f(m[e] - base);
+        f[e] = exp2f(m[e] - base);
         m[e] = next;
         p[e] = exp2f(p[e] - base);
         p[2 + e] = exp2f(p[2 + e] - base);
-        l[e] = l[e] * f + (p[e] + p[2 + e]);
+        l[e] = l[e] * f[e] + (p[e] + p[2 + e]);
+        f[e] *= grow;
+      }
+      if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
 #pragma unroll
-        for (int i = 0; i < kOut; ++i) { oc[i][e] *= f; oc[i][2 + e] *= f; }
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) oc[i][e] *= f[e & 1];
       }
       // P^T fragments: the probabilities (times the values' scales), transposed from keys x heads
       uint32_t pa[L::kP], pb[L::kP], f0[L::kP], f1[L::kP];
-      split<L::kP>(p[0] * vs0, p[1] * vs0, pa);
-      split<L::kP>(p[2] * vs1, p[3] * vs1, pb);
+      split<L::kP, kHalf>(p[0] * vs0, p[1] * vs0, pa);
+      split<L::kP, kHalf>(p[2] * vs1, p[3] * vs1, pb);
 #pragma unroll
       for (int c = 0; c < L::kP; ++c) { f0[c] = transpose8x8(pa[c]); f1[c] = transpose8x8(pb[c]); }
       // O^T += V^T P^T
-      int done = 0;
-#pragma unroll
-      for (int j = 0; j < kVJ; ++j) {
-        uint32_t vw[4][L::kC][kVE / 2];
+      if constexpr (kHalf) {
+        // rows are paired byte by byte before they are widened: half the permutes
+        constexpr int kWords = D / 32;               // words of four dims per lane and row
+        uint32_t vb[4][kWords];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int r = 2 * t + (x & 1) + (x >> 1) * 8;
           if constexpr (kChunks >= 8) {
-            const int c = (g + 8 * j) ^ swizzle_v<kChunks>(r);
-            chunk_to_bf16<C, L::kC, kE>(*reinterpret_cast<const uint4*>(vt + r * L::kRow + c * 16), vw[x]);
-          } else {                               // 64 dims of 8 bits: eight bytes of a chunk
-            const int c = (g >> 1) ^ swizzle_v<kChunks>(r);
-            const uint2 half = *reinterpret_cast<const uint2*>(vt + r * L::kRow + c * 16 + (g & 1) * 8);
-            float fa[4], fb[4];
-            codes_to_float<C>(half.x, fa);
-            codes_to_float<C>(half.y, fb);
-            vw[x][0][0] = pack_bf16(fa[0], fa[1]); vw[x][0][1] = pack_bf16(fa[2], fa[3]);
-            vw[x][0][2] = pack_bf16(fb[0], fb[1]); vw[x][0][3] = pack_bf16(fb[2], fb[3]);
+            const uint4 u = *reinterpret_cast<const uint4*>(vt + r * L::kRow + (g ^ swizzle_v<kChunks>(r)) * 16);
+            vb[x][0] = u.x; vb[x][1] = u.y; vb[x][2] = u.z; vb[x][3] = u.w;
+          } else {                                   // 64 dims: eight bytes of a chunk
+            const uint2 u = *reinterpret_cast<const uint2*>(vt + r * L::kRow + ((g >> 1) ^ swizzle_v<kChunks>(r)) * 16 + (g & 1) * 8);
+            vb[x][0] = u.x; vb[x][1] = u.y;
           }
         }
 #pragma unroll
-        for (int i = 0; i < kVE / 2; ++i) {
+        for (int i = 0; i < kWords; ++i)
 #pragma unroll
-          for (int vc = L::kC - 1; vc >= 0; --vc) {
-            const uint32_t fr[4] = {__byte_perm(vw[0][vc][i], vw[1][vc][i], 0x5410), __byte_perm(vw[0][vc][i], vw[1][vc][i], 0x7632),
-                                    __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x5410), __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x7632)};
+          for (int k = 0; k < 2; ++k) {
+            uint32_t fr[4];
+            codes_to_half<C>(__byte_perm(vb[0][i], vb[1][i], k ? 0x7362 : 0x5140), fr[0], fr[1]);
+            codes_to_half<C>(__byte_perm(vb[2][i], vb[3][i], k ? 0x7362 : 0x5140), fr[2], fr[3]);
 #pragma unroll
-            for (int pc = L::kP - 1; pc >= 0; --pc)
-              if (vc + pc <= 2) mma_bf16(oc[done], fr, f0[pc], f1[pc]);
+            for (int pc = L::kP - 1; pc >= 0; --pc) mma_f16(oc[2 * i + k], fr, f0[pc], f1[pc]);
           }
-          ++done;
+      } else {
+#pragma unroll
+        for (int j = 0; j < kVJ; ++j) {
+          uint32_t vw[4][L::kC][kVE / 2];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int r = 2 * t + (x & 1) + (x >> 1) * 8;
+            const int c = (g + 8 * j) ^ swizzle_v<kChunks>(r);
+            chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(vt + r * L::kRow + c * 16), vw[x]);
+          }
+#pragma unroll
+          for (int i = 0; i < kVE / 2; ++i)
+#pragma unroll
+            for (int vc = L::kC - 1; vc >= 0; --vc) {
+              const uint32_t fr[4] = {__byte_perm(vw[0][vc][i], vw[1][vc][i], 0x5410), __byte_perm(vw[0][vc][i], vw[1][vc][i], 0x7632),
+                                      __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x5410), __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x7632)};
+#pragma unroll
+              for (int pc = L::kP - 1; pc >= 0; --pc)
+                if (vc + pc <= 2) mma_bf16(oc[j * (kVE / 2) + i], fr, f0[pc], f1[pc]);
+            }
         }
       }
     }
@@ -429,17 +515,26 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) top[e] = fmaxf(top[e], wm[i * kHeads + 2 * t + e]);
         f[e] = m[e] == -INFINITY ? 0.f : exp2f(m[e] - top[e]);
+        if constexpr (kHalf) f[e] *= v_ref * (1.f / 16384.f);
       }
 #pragma unroll
-      for (int i = 0; i < kOut; ++i)
+      for (int round = 0; round < kWarps / kSlots; ++round) {            // in turn, so that the merge fits beside the ring
+        if (warp / kSlots == round) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (2 * t + e >= a.group) continue;
-          const int j = i / (kVE / 2), k = i % (kVE / 2);
-          const int dim = (kChunks >= 8 ? (g + 8 * j) * kE : g * kVE) + 2 * k;
-          *reinterpret_cast<float2*>(obuf + (warp * a.group + 2 * t + e) * D + dim) = make_float2(oc[i][e] * f[e], oc[i][2 + e] * f[e]);
+          for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              if (2 * t + e >= a.group) continue;
+              const int j = i / (kVE / 2), k = i % (kVE / 2);
+              const int dim = (kChunks >= 8 ? (g + 8 * j) * kE : g * kVE) + 2 * k;
+              float2* o = reinterpret_cast<float2*>(obuf + ((warp % kSlots) * a.group + 2 * t + e) * D + dim);
+              float2 v = make_float2(oc[i][e] * f[e], oc[i][2 + e] * f[e]);
+              if (round > 0) { const float2 old = *o; v.x += old.x; v.y += old.y; }
+              *o = v;
+            }
         }
-      __syncthreads();
+        __syncthreads();
+      }
       const bool whole = complete && first_part;
       const size_t head0 = ((size_t)cur.b * w.kv_heads + cur.h) * a.group;
       float* part = a.part + ((size_t)blockIdx.x * 2 + (first_part ? 1 : 0)) * a.group * (D + 2);
@@ -452,8 +547,9 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
         for (int i = 0; i < kWarps; ++i) {
           const float mi = wm[i * kHeads + hd];
           sum += mi == -INFINITY ? 0.f : wl[i * kHeads + hd] * exp2f(mi - big);
-          o += obuf[i * a.group * D + x];
         }
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) o += obuf[i * a.group * D + x];
         if (whole) {
           if (!cur.bad) {
             static_cast<T*>(a.out)[head0 * D + x] = (T)(sum == 0.f ? 0.f : o / sum);
@@ -485,7 +581,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
 // Joins the parts of the (sequence, KV head) that begins in block blockIdx.x and ends in a later one.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const DecodeArgs a, int kv_heads) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  begin();
   const int c0 = blockIdx.x;
   const int4 d = a.desc[c0];
   if (d.x < 0) return;
@@ -526,20 +622,11 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
   const size_t smem = L::smem(c->group);
   static BuzzSmemOptIn opt_in;
   if (cudaError_t e = opt_in.ensure(paged_decode_kernel<T, C, D>, smem); e != cudaSuccess) return e;
-  paged_decode_kernel<T, C, D><<<n, L::kThreads, smem, stream>>>(c->view(layer), a);
-  if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  if (cudaError_t e = buzz_launch_chained(paged_decode_kernel<T, C, D>, dim3(n), L::kThreads, smem, stream, c->view(layer), a); e != cudaSuccess)
+    return e;
   c->launches += 1;
   if (tiles <= L::kWarps) return cudaSuccess;      // one unit per (sequence, KV head): nothing is ever split
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n);
-  cfg.blockDim = dim3(256);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D>, (const DecodeArgs)a, c->sh.kv_heads);
+  cudaError_t e = buzz_launch_chained(paged_join_kernel<T, D>, dim3(n), 256u, 0, stream, a, c->sh.kv_heads);
   if (e == cudaSuccess) c->launches += 1;
   return e;
 }

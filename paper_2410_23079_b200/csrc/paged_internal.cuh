@@ -53,7 +53,31 @@ struct CacheBF16 { static constexpr int kSize = 2; static constexpr bool kScaled
 struct CacheE4M3 { static constexpr int kSize = 1; static constexpr bool kScaled = true; static constexpr float kTop = 448.f; };
 struct CacheI8 { static constexpr int kSize = 1; static constexpr bool kScaled = true; static constexpr float kTop = 127.f; };
 
+// Every kernel of the paged cache is launched so that it may be set up while the kernel before it in the
+// stream drains (programmatic dependent launch), and begins with buzz_paged_dev::begin(), which waits for
+// that kernel's end: the launch latency is hidden, the order of the stream is kept. The wait is made by
+// every block of every such kernel, so that the end of one implies the end of all before it.
+template <typename... P, typename... A>
+inline cudaError_t buzz_launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 namespace buzz_paged_dev {
+
+__device__ __forceinline__ void begin() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 
 // Two e4m3 codes (low byte first) as fp32; exact.
 __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t codes) {

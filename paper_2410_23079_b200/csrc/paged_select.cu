@@ -8,9 +8,9 @@
 // the border are chosen or left out as a whole, and in fp32 the order of a sum would decide that.
 //
 // score_kernel: a block takes a run of pages of one (sequence, KV head); a page belongs to some lanes of
-//   a warp, 16 bytes each. Scores are left as unsigned keys that sort like the scores.
-// pick_kernel: one block per (sequence, KV head); radix selection of the top-th largest key, eight bits
-//   a pass, then one ordered pass that writes the pages ascending (equal keys: the lowest pages).
+//   a warp, 16 bytes each, and eight pages' loads are under way at once. Scores are left as unsigned keys that sort like the scores.
+// pick_kernel: one block per (sequence, KV head) finds the top-th largest key and writes the pages
+//   ascending (equal keys: the lowest pages).
 #include "paged_internal.cuh"
 
 namespace {
@@ -33,68 +33,121 @@ __device__ __forceinline__ unsigned long long ordered_key(double x) {
 }
 
 constexpr int kScoreWarps = 8;
+constexpr int kBatch = 8;            // pages of a lane group whose bounds are under way together
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView w, const SelectArgs a, int pages_per_block) {
-  constexpr int kE = 16 / sizeof(T);
-  constexpr int kChunks = 2 * D / kE;                       // 16-byte chunks of a page's bounds
-  constexpr int kLanes = kChunks < 32 ? kChunks : 32;       // lanes of a page
-  constexpr int kCL = kChunks / kLanes;                     // chunks per lane
-  constexpr int kPages = 32 / kLanes;                       // pages a warp works on at a time
+struct ScorePlan {
+  static constexpr int kE = 16 / sizeof(T);
+  static constexpr int kChunks = 2 * D / kE;                       // 16-byte chunks of a page's bounds
+  static constexpr int kLanes = kChunks < 32 ? kChunks : 32;       // lanes of a page
+  static constexpr int kCL = kChunks / kLanes;                     // chunks per lane
+  static constexpr int kPages = 32 / kLanes;                       // lane groups of a warp
+  static constexpr int kPerBlock = kScoreWarps * kPages * kBatch;
+};
+
+template <typename T>
+__device__ __forceinline__ void widen(const uint4& u, float (&x)[16 / sizeof(T)]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    else x[i] = __uint_as_float(w[i]);
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView w, const SelectArgs a) {
+  using L = ScorePlan<T, D>;
+  constexpr int kE = L::kE, kLanes = L::kLanes, kCL = L::kCL;
+  begin();
   const int b = blockIdx.z, h = blockIdx.y;
   const int len = a.lens[b];
   if (len < 0 || len > a.max_len) return;                   // the pick records it
   const int count = (len + (1 << w.page_log2) - 1) >> w.page_log2;
   if (count <= a.sink + a.recent + a.top) return;
-  const int end = min(count - a.recent, a.sink + (int)(blockIdx.x + 1) * pages_per_block);
-  const int begin = a.sink + blockIdx.x * pages_per_block;
-  if (begin >= end) return;
   const int warp = threadIdx.x / 32, wl = threadIdx.x & 31, lane = wl % kLanes, sub = wl / kLanes;
+  const int end = count - a.recent;
+  const int p0 = a.sink + blockIdx.x * L::kPerBlock + warp * (L::kPages * kBatch) + sub * kBatch;     // this lane group's pages
+  if (a.sink + (int)blockIdx.x * L::kPerBlock + warp * (L::kPages * kBatch) >= end) return;           // all of the warp's
+  // the pages' bounds, all under way before the first is used
+  uint4 raw[kBatch][kCL];
+  int mine = -1;                                            // lane i of a group looks up page i
+  if (lane < kBatch && p0 + lane < end) {
+    mine = a.table[(int64_t)b * a.table_stride + p0 + lane];
+    if (mine < 0 || mine >= w.pages) {
+      buzz_set_status(w.status, BUZZ_ERR_INVALID, b, mine);
+      mine = -1;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i) {
+    const int page = __shfl_sync(0xffffffffu, mine, i, kLanes);
+    const uint4* src = reinterpret_cast<const uint4*>(w.bounds) + ((size_t)max(page, 0) * w.kv_heads + h) * L::kChunks + lane;
+#pragma unroll
+    for (int c = 0; c < kCL; ++c) raw[i][c] = page >= 0 ? src[c * kLanes] : make_uint4(0, 0, 0, 0);
+  }
   double qs[kCL][kE];
 #pragma unroll
   for (int c = 0; c < kCL; ++c) {
-    const int d0 = (lane + c * kLanes) * kE % D;
-    const bool high = (lane + c * kLanes) * kE >= D;        // the second half of the bounds is the largest values
+    const int at = lane + c * kLanes;
+    const bool high = at * kE >= D;                         // the second half of the bounds is the largest values
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + ((size_t)b * w.kv_heads + h) * a.group * D) + at % (D / kE);
 #pragma unroll
     for (int e = 0; e < kE; ++e) qs[c][e] = 0.0;
     for (int g = 0; g < a.group; ++g) {
-      const T* q = static_cast<const T*>(a.q) + (((size_t)b * w.kv_heads + h) * a.group + g) * D + d0;
+      float x[kE];
+      widen<T>(q[g * (D / kE)], x);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        const double x = (double)(float)q[e];
-        qs[c][e] += high ? (x < 0.0 ? 0.0 : x) : (x < 0.0 ? x : 0.0);
-      }
+      for (int e = 0; e < kE; ++e) qs[c][e] += (double)(high ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] < 0.f ? x[e] : 0.f));
     }
   }
-  unsigned long long* keys = a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages;
-  for (int p0 = begin + warp * kPages; p0 < end; p0 += kScoreWarps * kPages) {
-    const int lp = p0 + sub;
-    double s = 0.0;
-    if (lp < end) {
-      const int page = a.table[(int64_t)b * a.table_stride + lp];
-      if (page >= 0 && page < w.pages) {
-        const T* bnd = reinterpret_cast<const T*>(w.bounds) + ((size_t)page * w.kv_heads + h) * 2 * D;
+  double s[kBatch];
 #pragma unroll
-        for (int c = 0; c < kCL; ++c)
+  for (int i = 0; i < kBatch; ++i) {
+    s[i] = 0.0;
 #pragma unroll
-          for (int e = 0; e < kE; ++e) s += qs[c][e] * (double)(float)bnd[(lane + c * kLanes) * kE + e];
-      } else {
-        if (lane == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, b, page);
-        s = -INFINITY;
-      }
+    for (int c = 0; c < kCL; ++c) {
+      float x[kE];
+      widen<T>(raw[i][c], x);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) s[i] += qs[c][e] * (double)x[e];
     }
-#pragma unroll
-    for (int off = kLanes / 2; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    if (lane == 0 && lp < end) keys[lp] = ordered_key(s);
   }
+  // sums over the lane group, eight pages at once: each step halves the pages a lane holds
+  int off = kLanes / 2;
+#pragma unroll
+  for (int n = kBatch / 2; n >= 1; n >>= 1) {
+    const bool up = lane & off;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const double give = up ? s[i] : s[i + n], keep = up ? s[i + n] : s[i];
+      s[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+    }
+    off >>= 1;
+  }
+#pragma unroll
+  for (; off > 0; off >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], off);
+  constexpr int kRest = kLanes / kBatch;                    // lanes that now hold one page's sum
+  const int i = lane / kRest;
+  const int page = __shfl_sync(0xffffffffu, mine, i, kLanes);
+  if (lane % kRest == 0 && p0 + i < end)
+    a.keys[((size_t)b * w.kv_heads + h) * a.max_pages + p0 + i] = page >= 0 ? ordered_key(s[0]) : 0;      // a bad page is below all others
 }
 
-constexpr int kPickThreads = 512;
+// The pick: a block per (sequence, KV head). A histogram of kBins equal bins over the keys' range, then over
+// the bin that holds the border, until that bin is taken whole; two or three rounds where the scores spread.
+constexpr int kPickThreads = 1024;
+constexpr int kPickWarps = kPickThreads / 32;
+constexpr int kBins = 2 * kPickThreads;
+constexpr int kHeld = 8;             // keys a thread keeps in registers; more are read again each round
 
 __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, const SelectArgs a) {
-  __shared__ int hist[256];
-  __shared__ int warp_cnt[2][kPickThreads / 32];
-  __shared__ int pick_bin, pick_rest;
+  typedef unsigned long long u64;
+  __shared__ int hist[kBins];
+  __shared__ u64 ends[2][kPickWarps];
+  __shared__ int cnt[2][kPickWarps];
+  __shared__ int border, border_rest, border_count;
+  begin();
   const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
   const int len = a.lens[b];
   if (len < 0 || len > a.max_len) {
@@ -111,75 +164,106 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, c
   for (int i = tid; i < a.sink; i += kPickThreads) out[i] = i;
   for (int i = tid; i < a.recent; i += kPickThreads) out[a.sink + a.top + i] = count - a.recent + i;
   if (a.top == 0) return;
-  const unsigned long long* keys = a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages;
-  const int first = a.sink, end = count - a.recent;
-  // the top-th largest key: its leading bytes one after the other
-  unsigned long long prefix = 0, mask = 0;
-  int rest = a.top;                              // how many of the keys that share the prefix are kept
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kPickThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = first + tid; i < end; i += kPickThreads) {
-      const unsigned long long key = keys[i];
-      if ((key & mask) == prefix) atomicAdd(&hist[(int)(key >> shift) & 255], 1);
-    }
-    __syncthreads();
-    if (tid == 0) {
-      int above = 0, bin = 255;
-      for (; bin > 0; --bin) {
-        if (above + hist[bin] >= rest) break;
-        above += hist[bin];
-      }
-      pick_bin = bin;
-      pick_rest = rest - above;
-    }
-    __syncthreads();
-    prefix |= (unsigned long long)pick_bin << shift;
-    mask |= 255ull << shift;
-    rest = pick_rest;
+  // thread t holds a run of consecutive pages, so that ranks in page order follow from one scan
+  const u64* keys = a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages + a.sink;
+  const int n = count - a.recent - a.sink, per = (n + kPickThreads - 1) / kPickThreads;
+  const int lo = min(tid * per, n), mine = min(per, n - lo);
+  u64 held[kHeld];
+  u64 small = ~0ull, large = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = i < mine ? keys[lo + i] : 0;
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (i < mine) f(held[i], i);
+    for (int i = kHeld; i < mine; ++i) f(keys[lo + i], i);
+  };
+  each([&](u64 k, int) { small = min(small, k); large = max(large, k); });
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    small = min(small, __shfl_xor_sync(0xffffffffu, small, off));
+    large = max(large, __shfl_xor_sync(0xffffffffu, large, off));
   }
-  // ordered pass: keys above the prefix, and the first `rest` equal to it
-  int done = 0, equal = 0;                       // written so far, equal keys met so far
-  for (int i0 = first; i0 < end; i0 += kPickThreads) {
-    const int i = i0 + tid;
-    const unsigned long long key = i < end ? keys[i] : 0;
-    const bool is_eq = i < end && key == prefix, is_above = i < end && key > prefix;
-    const unsigned beq = __ballot_sync(0xffffffffu, is_eq);
-    if (lane == 0) warp_cnt[0][warp] = __popc(beq);
-    __syncthreads();
-    int eq_before = equal, eq_all = 0;
-    for (int x = 0; x < kPickThreads / 32; ++x) {
-      if (x < warp) eq_before += warp_cnt[0][x];
-      eq_all += warp_cnt[0][x];
-    }
-    const bool take = is_above || (is_eq && eq_before + __popc(beq & ((1u << lane) - 1)) < rest);
-    const unsigned bt = __ballot_sync(0xffffffffu, take);
-    if (lane == 0) warp_cnt[1][warp] = __popc(bt);
-    __syncthreads();
-    int at = done, all = 0;
-    for (int x = 0; x < kPickThreads / 32; ++x) {
-      if (x < warp) at += warp_cnt[1][x];
-      all += warp_cnt[1][x];
-    }
-    if (take) out[a.sink + at + __popc(bt & ((1u << lane) - 1))] = i;
-    done += all;
-    equal += eq_all;
+  if (lane == 0) { ends[0][warp] = small; ends[1][warp] = large; }
+  hist[tid] = hist[tid + kPickThreads] = 0;
+  __syncthreads();
+  small = ends[0][lane];
+  large = ends[1][lane];
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    small = min(small, __shfl_xor_sync(0xffffffffu, small, off));
+    large = max(large, __shfl_xor_sync(0xffffffffu, large, off));
   }
+  u64 base = small, span = large - small;        // keys base .. base + span hold the border
+  int rest = a.top;                              // how many of them are kept
+  u64 above;                                     // keys from here on are kept
+  for (;;) {
+    const int shift = max(0, 64 - __clzll((long long)span) - 11);
+    each([&](u64 k, int) { if (k - base <= span) atomicAdd(&hist[(int)((k - base) >> shift)], 1); });
+    __syncthreads();
+    // bins from the top: thread t has bins kBins - 1 - 2t and the one below it
+    const int c0 = hist[kBins - 1 - 2 * tid], c1 = hist[kBins - 2 - 2 * tid];
+    int incl = c0 + c1;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += o;
+    }
+    if (lane == 31) cnt[0][warp] = incl;
+    __syncthreads();
+    hist[kBins - 1 - 2 * tid] = hist[kBins - 2 - 2 * tid] = 0;
+    int over = incl - c0 - c1;
+    for (int x = 0; x < kPickWarps; ++x) over += x < warp ? cnt[0][x] : 0;
+    if (over < rest && rest <= over + c0 + c1) {
+      const bool second = rest > over + c0;
+      border = kBins - 1 - 2 * tid - (second ? 1 : 0);
+      border_rest = rest - over - (second ? c0 : 0);
+      border_count = second ? c1 : c0;
+    }
+    __syncthreads();
+    base += (u64)border << shift;
+    rest = border_rest;
+    span = (1ull << shift) - 1;
+    if (border_count == rest) { above = base; rest = 0; break; }
+    if (shift == 0) { above = base + 1; break; }             // equal keys: the first `rest` of them
+  }
+  // ranks in page order (above wraps to 0 only if base is the largest key there is: then nothing is above)
+  const bool none_above = rest > 0 && above == 0;
+  int kept = 0, equal = 0;
+  each([&](u64 k, int) {
+    kept += !none_above && k >= above;
+    equal += rest > 0 && k == base;
+  });
+  int ik = kept, ie = equal;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, ik, off), y = __shfl_up_sync(0xffffffffu, ie, off);
+    if (lane >= off) { ik += x; ie += y; }
+  }
+  if (lane == 31) { cnt[0][warp] = ik; cnt[1][warp] = ie; }
+  __syncthreads();
+  int at = ik - kept, eq = ie - equal;
+  for (int x = 0; x < kPickWarps; ++x) { at += x < warp ? cnt[0][x] : 0; eq += x < warp ? cnt[1][x] : 0; }
+  at += min(eq, rest);
+  each([&](u64 k, int i) {
+    bool take = !none_above && k >= above;
+    if (rest > 0 && k == base) take = eq++ < rest;
+    if (take) out[a.sink + at++] = a.sink + lo + i;
+  });
 }
 
 template <typename T, int D>
 cudaError_t launch(buzz_paged* c, int layer, const SelectArgs& a, cudaStream_t s) {
   const int middle = a.max_pages - a.sink - a.recent;
   if (a.top > 0 && middle > a.top) {
-    const int per = 64;
+    const int per = ScorePlan<T, D>::kPerBlock;
     const dim3 grid((middle + per - 1) / per, c->sh.kv_heads, a.batch);
-    score_kernel<T, D><<<grid, kScoreWarps * 32, 0, s>>>(c->view(layer), a, per);
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+    if (cudaError_t e = buzz_launch_chained(score_kernel<T, D>, grid, kScoreWarps * 32u, 0, s, c->view(layer), a); e != cudaSuccess) return e;
     c->launches += 1;
   }
-  pick_kernel<<<dim3(c->sh.kv_heads, a.batch), kPickThreads, 0, s>>>(c->view(layer), a);
-  c->launches += 1;
-  return cudaGetLastError();
+  const cudaError_t e = buzz_launch_chained(pick_kernel, dim3(c->sh.kv_heads, a.batch), (unsigned)kPickThreads, 0, s, c->view(layer), a);
+  if (e == cudaSuccess) c->launches += 1;
+  return e;
 }
 
 }  // namespace
