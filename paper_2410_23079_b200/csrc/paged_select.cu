@@ -32,7 +32,7 @@ __device__ __forceinline__ unsigned long long ordered_key(double x) {
   return (u >> 63) ? ~u : u | 0x8000000000000000ull;
 }
 
-constexpr int kScoreWarps = 8;
+constexpr int kScoreWarps = 4;
 constexpr int kBatch = 8;            // pages of a lane group whose bounds are under way together
 
 template <typename T, int D>
@@ -42,7 +42,8 @@ struct ScorePlan {
   static constexpr int kLanes = kChunks < 32 ? kChunks : 32;       // lanes of a page
   static constexpr int kCL = kChunks / kLanes;                     // chunks per lane
   static constexpr int kPages = 32 / kLanes;                       // lane groups of a warp
-  static constexpr int kPerBlock = kScoreWarps * kPages * kBatch;
+  static constexpr int kBatches = kLanes / kBatch;                 // a lane looks up one page of its group
+  static constexpr int kPerBlock = kScoreWarps * 32;
 };
 
 template <typename T>
@@ -65,88 +66,104 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView
   if (len < 0 || len > a.max_len) return;                   // the pick records it
   const int count = (len + (1 << w.page_log2) - 1) >> w.page_log2;
   if (count <= a.sink + a.recent + a.top) return;
-  const int warp = threadIdx.x / 32, wl = threadIdx.x & 31, lane = wl % kLanes, sub = wl / kLanes;
-  const int end = count - a.recent;
-  const int p0 = a.sink + blockIdx.x * L::kPerBlock + warp * (L::kPages * kBatch) + sub * kBatch;     // this lane group's pages
-  if (a.sink + (int)blockIdx.x * L::kPerBlock + warp * (L::kPages * kBatch) >= end) return;           // all of the warp's
-  // the pages' bounds, all under way before the first is used
-  uint4 raw[kBatch][kCL];
-  int mine = -1;                                            // lane i of a group looks up page i
-  if (lane < kBatch && p0 + lane < end) {
+  const int tid = threadIdx.x, warp = tid / 32, wl = tid & 31, lane = wl % kLanes, sub = wl / kLanes;
+  const int end = count - a.recent, block0 = a.sink + blockIdx.x * L::kPerBlock;
+  if (block0 >= end) return;
+  // lane i of a group looks up page i of the group's run
+  const int p0 = block0 + warp * 32 + sub * kLanes;
+  int mine = -1;
+  if (p0 + lane < end) {
     mine = a.table[(int64_t)b * a.table_stride + p0 + lane];
     if (mine < 0 || mine >= w.pages) {
       buzz_set_status(w.status, BUZZ_ERR_INVALID, b, mine);
       mine = -1;
     }
   }
-#pragma unroll
-  for (int i = 0; i < kBatch; ++i) {
-    const int page = __shfl_sync(0xffffffffu, mine, i, kLanes);
-    const uint4* src = reinterpret_cast<const uint4*>(w.bounds) + ((size_t)max(page, 0) * w.kv_heads + h) * L::kChunks + lane;
-#pragma unroll
-    for (int c = 0; c < kCL; ++c) raw[i][c] = page >= 0 ? src[c * kLanes] : make_uint4(0, 0, 0, 0);
+  // the group's queries by sign, once per block
+  __shared__ double qsum[2 * D];
+  for (int i = tid; i < 2 * D; i += kScoreWarps * 32) {
+    const T* q = static_cast<const T*>(a.q) + ((size_t)b * w.kv_heads + h) * a.group * D + i % D;
+    double sum = 0.0;
+    for (int g = 0; g < a.group; ++g) {
+      const float x = (float)q[g * D];
+      sum += (double)((x < 0.f) == (i < D) || x != x ? x : 0.f);    // the first half of the bounds is the smallest values
+    }
+    qsum[i] = sum;
   }
+  uint4 raw[kBatch][kCL];
+  auto fetch = [&](int batch) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int page = __shfl_sync(0xffffffffu, mine, batch * kBatch + i, kLanes);
+      const uint4* src = reinterpret_cast<const uint4*>(w.bounds) + ((size_t)max(page, 0) * w.kv_heads + h) * L::kChunks + lane;
+#pragma unroll
+      for (int c = 0; c < kCL; ++c) raw[i][c] = page >= 0 ? src[c * kLanes] : make_uint4(0, 0, 0, 0);
+    }
+  };
+  fetch(0);
+  __syncthreads();
   double qs[kCL][kE];
 #pragma unroll
-  for (int c = 0; c < kCL; ++c) {
-    const int at = lane + c * kLanes;
-    const bool high = at * kE >= D;                         // the second half of the bounds is the largest values
-    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + ((size_t)b * w.kv_heads + h) * a.group * D) + at % (D / kE);
+  for (int c = 0; c < kCL; ++c)
 #pragma unroll
-    for (int e = 0; e < kE; ++e) qs[c][e] = 0.0;
-    for (int g = 0; g < a.group; ++g) {
-      float x[kE];
-      widen<T>(q[g * (D / kE)], x);
+    for (int e = 0; e < kE; ++e) qs[c][e] = qsum[(lane + c * kLanes) * kE + e];
+#pragma unroll 1
+  for (int batch = 0; batch < L::kBatches; ++batch) {
+    if (block0 + warp * 32 + batch * kBatch >= end) break;    // nothing left for any group of the warp
+    double s[kBatch];
 #pragma unroll
-      for (int e = 0; e < kE; ++e) qs[c][e] += (double)(high ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] < 0.f ? x[e] : 0.f));
+    for (int i = 0; i < kBatch; ++i) {
+      s[i] = 0.0;
+#pragma unroll
+      for (int c = 0; c < kCL; ++c) {
+        float x[kE];
+        widen<T>(raw[i][c], x);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) s[i] += qs[c][e] * (double)x[e];
+      }
     }
-  }
-  double s[kBatch];
+    if (batch + 1 < L::kBatches) fetch(batch + 1);
+    // sums over the lane group, eight pages at once: each step halves the pages a lane holds
+    int off = kLanes / 2;
 #pragma unroll
-  for (int i = 0; i < kBatch; ++i) {
-    s[i] = 0.0;
+    for (int n = kBatch / 2; n >= 1; n >>= 1) {
+      const bool up = lane & off;
 #pragma unroll
-    for (int c = 0; c < kCL; ++c) {
-      float x[kE];
-      widen<T>(raw[i][c], x);
-#pragma unroll
-      for (int e = 0; e < kE; ++e) s[i] += qs[c][e] * (double)x[e];
+      for (int i = 0; i < n; ++i) {
+        const double give = up ? s[i] : s[i + n], keep = up ? s[i + n] : s[i];
+        s[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+      }
+      off >>= 1;
     }
+#pragma unroll
+    for (; off > 0; off >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], off);
+    constexpr int kRest = kLanes / kBatch;                    // lanes that now hold one page's sum
+    const int i = batch * kBatch + lane / kRest;
+    const int page = __shfl_sync(0xffffffffu, mine, i, kLanes);
+    if (lane % kRest == 0 && p0 + i < end)
+      a.keys[((size_t)b * w.kv_heads + h) * a.max_pages + p0 + i] = page >= 0 ? ordered_key(s[0]) : 0;      // a bad page is below all others
   }
-  // sums over the lane group, eight pages at once: each step halves the pages a lane holds
-  int off = kLanes / 2;
-#pragma unroll
-  for (int n = kBatch / 2; n >= 1; n >>= 1) {
-    const bool up = lane & off;
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const double give = up ? s[i] : s[i + n], keep = up ? s[i + n] : s[i];
-      s[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
-    }
-    off >>= 1;
-  }
-#pragma unroll
-  for (; off > 0; off >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], off);
-  constexpr int kRest = kLanes / kBatch;                    // lanes that now hold one page's sum
-  const int i = lane / kRest;
-  const int page = __shfl_sync(0xffffffffu, mine, i, kLanes);
-  if (lane % kRest == 0 && p0 + i < end)
-    a.keys[((size_t)b * w.kv_heads + h) * a.max_pages + p0 + i] = page >= 0 ? ordered_key(s[0]) : 0;      // a bad page is below all others
 }
 
-// The pick: a block per (sequence, KV head). A histogram of kBins equal bins over the keys' range, then over
-// the bin that holds the border, until that bin is taken whole; two or three rounds where the scores spread.
+// The pick: a block per (sequence, KV head). A histogram of kBins equal bins over the keys' range finds the
+// bin that holds the border; its keys (a handful where the scores spread) are ranked against one another,
+// and the one of the wanted rank is the last that is kept. A crowded bin is cut into kBins once more, down
+// to single values; pages of one value are ranked by their number.
 constexpr int kPickThreads = 1024;
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kBins = 2 * kPickThreads;
-constexpr int kHeld = 8;             // keys a thread keeps in registers; more are read again each round
+constexpr int kHeld = 8;             // keys a thread keeps in registers; more are read again each time
+constexpr int kRanked = 256;         // keys that are ranked directly
 
 __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, const SelectArgs a) {
   typedef unsigned long long u64;
   __shared__ int hist[kBins];
   __shared__ u64 ends[2][kPickWarps];
-  __shared__ int cnt[2][kPickWarps];
-  __shared__ int border, border_rest, border_count;
+  __shared__ u64 cand[kRanked];
+  __shared__ int cand_at[kRanked];
+  __shared__ int cnt[kPickWarps];
+  __shared__ int border, border_rest, border_count, cand_n, last_at;
+  __shared__ u64 last_key;
   begin();
   const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
   const int len = a.lens[b];
@@ -164,19 +181,18 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, c
   for (int i = tid; i < a.sink; i += kPickThreads) out[i] = i;
   for (int i = tid; i < a.recent; i += kPickThreads) out[a.sink + a.top + i] = count - a.recent + i;
   if (a.top == 0) return;
-  // thread t holds a run of consecutive pages, so that ranks in page order follow from one scan
+  // key i of the thread is that of page i * kPickThreads + tid of the middle
   const u64* keys = a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages + a.sink;
-  const int n = count - a.recent - a.sink, per = (n + kPickThreads - 1) / kPickThreads;
-  const int lo = min(tid * per, n), mine = min(per, n - lo);
+  const int n = count - a.recent - a.sink;
   u64 held[kHeld];
   u64 small = ~0ull, large = 0;
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) held[i] = i < mine ? keys[lo + i] : 0;
+  for (int i = 0; i < kHeld; ++i) held[i] = i * kPickThreads + tid < n ? keys[i * kPickThreads + tid] : 0;
   auto each = [&](auto&& f) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
-      if (i < mine) f(held[i], i);
-    for (int i = kHeld; i < mine; ++i) f(keys[lo + i], i);
+      if (i * kPickThreads + tid < n) f(held[i], i * kPickThreads + tid);
+    for (int i = kHeld * kPickThreads + tid; i < n; i += kPickThreads) f(keys[i], i);
   };
   each([&](u64 k, int) { small = min(small, k); large = max(large, k); });
 #pragma unroll
@@ -186,6 +202,7 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, c
   }
   if (lane == 0) { ends[0][warp] = small; ends[1][warp] = large; }
   hist[tid] = hist[tid + kPickThreads] = 0;
+  if (tid == 0) cand_n = 0;
   __syncthreads();
   small = ends[0][lane];
   large = ends[1][lane];
@@ -195,10 +212,9 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, c
     large = max(large, __shfl_xor_sync(0xffffffffu, large, off));
   }
   u64 base = small, span = large - small;        // keys base .. base + span hold the border
-  int rest = a.top;                              // how many of them are kept
-  u64 above;                                     // keys from here on are kept
+  int rest = a.top, shift;                       // how many of them are kept
   for (;;) {
-    const int shift = max(0, 64 - __clzll((long long)span) - 11);
+    shift = max(0, 64 - __clzll((long long)span) - 11);
     each([&](u64 k, int) { if (k - base <= span) atomicAdd(&hist[(int)((k - base) >> shift)], 1); });
     __syncthreads();
     // bins from the top: thread t has bins kBins - 1 - 2t and the one below it
@@ -209,11 +225,10 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, c
       const int o = __shfl_up_sync(0xffffffffu, incl, off);
       if (lane >= off) incl += o;
     }
-    if (lane == 31) cnt[0][warp] = incl;
+    if (lane == 31) cnt[warp] = incl;
     __syncthreads();
     hist[kBins - 1 - 2 * tid] = hist[kBins - 2 - 2 * tid] = 0;
-    int over = incl - c0 - c1;
-    for (int x = 0; x < kPickWarps; ++x) over += x < warp ? cnt[0][x] : 0;
+    int over = incl - c0 - c1 + (int)__reduce_add_sync(0xffffffffu, lane < warp ? cnt[lane] : 0);
     if (over < rest && rest <= over + c0 + c1) {
       const bool second = rest > over + c0;
       border = kBins - 1 - 2 * tid - (second ? 1 : 0);
@@ -222,34 +237,74 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, c
     }
     __syncthreads();
     base += (u64)border << shift;
-    rest = border_rest;
     span = (1ull << shift) - 1;
-    if (border_count == rest) { above = base; rest = 0; break; }
-    if (shift == 0) { above = base + 1; break; }             // equal keys: the first `rest` of them
+    rest = border_rest;
+    if (border_count <= kRanked || shift == 0) break;
   }
-  // ranks in page order (above wraps to 0 only if base is the largest key there is: then nothing is above)
-  const bool none_above = rest > 0 && above == 0;
-  int kept = 0, equal = 0;
-  each([&](u64 k, int) {
-    kept += !none_above && k >= above;
-    equal += rest > 0 && k == base;
-  });
-  int ik = kept, ie = equal;
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, ik, off), y = __shfl_up_sync(0xffffffffu, ie, off);
-    if (lane >= off) { ik += x; ie += y; }
+  // the last key that is kept: the one of rank `rest` in the border's bin
+  if (border_count <= kRanked) {
+    each([&](u64 k, int i) {
+      if (k - base <= span) {
+        const int at = atomicAdd(&cand_n, 1);
+        cand[at] = k;
+        cand_at[at] = i;
+      }
+    });
+    __syncthreads();
+    const int c = border_count;
+    if (tid < c) {
+      int rank = 0;
+      for (int x = 0; x < c; ++x) rank += cand[x] > cand[tid] || (cand[x] == cand[tid] && cand_at[x] < cand_at[tid]);
+      if (rank == rest - 1) { last_key = cand[tid]; last_at = cand_at[tid]; }
+    }
+  } else {                                       // one value: the page of that rank among its pages
+    int seen = 0;
+    for (int i0 = 0; i0 < n; i0 += kPickThreads) {
+      const bool eq = i0 + tid < n && keys[i0 + tid] == base;
+      const unsigned bal = __ballot_sync(0xffffffffu, eq);
+      if (lane == 0) cnt[warp] = __popc(bal);
+      __syncthreads();
+      const int before = seen + (int)__reduce_add_sync(0xffffffffu, lane < warp ? cnt[lane] : 0) + __popc(bal & ((1u << lane) - 1));
+      seen += (int)__reduce_add_sync(0xffffffffu, cnt[lane]);
+      if (eq && before == rest - 1) { last_key = base; last_at = i0 + tid; }
+      __syncthreads();
+    }
   }
-  if (lane == 31) { cnt[0][warp] = ik; cnt[1][warp] = ie; }
   __syncthreads();
-  int at = ik - kept, eq = ie - equal;
-  for (int x = 0; x < kPickWarps; ++x) { at += x < warp ? cnt[0][x] : 0; eq += x < warp ? cnt[1][x] : 0; }
-  at += min(eq, rest);
-  each([&](u64 k, int i) {
-    bool take = !none_above && k >= above;
-    if (rest > 0 && k == base) take = eq++ < rest;
-    if (take) out[a.sink + at++] = a.sink + lo + i;
-  });
+  // the kept pages in order: ranks of kHeld rows of pages at a time (hist is free: a count per row and warp)
+  const u64 lk = last_key;
+  const int la = last_at;
+  int done = 0;
+  for (int r0 = 0; r0 * kPickThreads < n; r0 += kHeld) {
+    unsigned bal[kHeld];
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+      const int i = (r0 + r) * kPickThreads + tid;
+      u64 k = 0;
+      if (i < n) k = r0 == 0 ? held[r] : keys[i];
+      bal[r] = __ballot_sync(0xffffffffu, i < n && (k > lk || (k == lk && i <= la)));
+      if (lane == 0) hist[r * kPickWarps + warp] = __popc(bal[r]);
+    }
+    __syncthreads();
+    if (warp < kHeld) {                          // warp r: the counts of row r become ranks within it
+      const int v = hist[warp * kPickWarps + lane];
+      int incl = v;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += o;
+      }
+      hist[warp * kPickWarps + lane] = incl - v;
+      if (lane == 31) cnt[warp] = incl;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+      if (bal[r] >> lane & 1) out[a.sink + done + hist[r * kPickWarps + warp] + __popc(bal[r] & ((1u << lane) - 1))] = a.sink + (r0 + r) * kPickThreads + tid;
+      done += cnt[r];
+    }
+    __syncthreads();
+  }
 }
 
 template <typename T, int D>
