@@ -5,6 +5,27 @@
 
 namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+
+// All rows of a pool as bytes, in swizzled boxes of one tile.
+bool make_map(CUtensorMap* map, void* base, size_t rows, int row_bytes, int page_tokens) {
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)buzz_paged_box_bytes(row_bytes), (cuuint32_t)buzz_paged_box_rows(row_bytes, page_tokens)};
+  const cuuint32_t steps[2] = {1, 1};
+  return reinterpret_cast<EncodeTiledFn>(p)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                            box[0] == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 }  // namespace
 
 extern "C" {
@@ -28,6 +49,8 @@ int buzz_paged_create(buzz_paged_t* out, const buzz_paged_shape* s, const buzz_p
   if (!b->k || !b->v || !b->status || (scaled && (!b->k_scale || !b->v_scale))) return BUZZ_ERR_INVALID;
   if (!aligned16(b->k) || !aligned16(b->v) || !aligned16(b->k_scale) || !aligned16(b->v_scale) || !aligned16(b->bounds) || !aligned16(b->status))
     return BUZZ_ERR_INVALID;
+  const size_t rows = (size_t)s->layers * s->pages * s->kv_heads * s->page_tokens;
+  if ((double)s->layers * s->pages * s->kv_heads * s->page_tokens > 2147483647.0) return BUZZ_ERR_TOO_LARGE;   // a row is a 32-bit coordinate
   buzz_paged* c = new (std::nothrow) buzz_paged();
   if (!c) return BUZZ_ERR_INVALID;
   c->sh = *s;
@@ -44,6 +67,11 @@ int buzz_paged_create(buzz_paged_t* out, const buzz_paged_shape* s, const buzz_p
     c->sm_count = sms;
   else
     (void)cudaGetLastError();
+  if (!make_map(&c->k_map, b->k, rows, (int)(s->head_dim * c->csize), s->page_tokens) ||
+      !make_map(&c->v_map, b->v, rows, (int)(s->head_dim * c->csize), s->page_tokens)) {
+    delete c;
+    return BUZZ_ERR_CUDA;
+  }
   if (cudaMemset(b->status, 0, 4 * sizeof(int32_t)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     delete c;
     return BUZZ_ERR_CUDA;

@@ -2,15 +2,18 @@
 // one KV head's rows shared by up to eight query heads.
 //
 // The work is one pass over K and V, so HBM bounds it. All sequences' rows form one line of work in
-// units of kWarps tiles of 16 tokens (sequence, then KV head, then length), and a grid of one block per
-// SM cuts that line into equal stretches: however ragged the batch, every block reads the same amount. A
-// stretch may begin or end inside a (sequence, KV head); such parts are written as (max, sum, output)
-// to the workspace and joined by a second, small kernel in the order of the line.
+// units of kWarps tiles (sequence, then KV head, then length), and a grid of one block per SM cuts that
+// line into equal stretches: however ragged the batch, every block reads the same amount. A stretch may
+// begin or end inside a (sequence, KV head); such parts are written as (max, sum, output) to the
+// workspace and joined by a second, small kernel in the order of the line.
 //
-// A block's warps take the tiles of a unit in turn and are independent until their (sequence, KV head)
-// ends. Each keeps a ring of tiles in shared memory, filled by 16-byte asynchronous copies of its own
-// (no block barrier, and the next (sequence, KV head)'s rows are under way while one is finished).
-// Rows behind a sequence's end are filled with zeros, so nothing that a page holds there is multiplied.
+// One warp of a block looks pages up and fetches tiles by tensor copies (swizzled boxes that lie within a
+// page) into a ring per consumer warp; each of its lanes serves one tile of the next 32, so that look-ups
+// cost the consumers nothing. The consumer warps take the tiles of a unit in turn and are independent
+// until their (sequence, KV head) ends; the next one's rows are under way meanwhile. Rows behind a
+// sequence's end are overwritten with zeros before they are multiplied. (With every warp copying for
+// itself, 16 bytes a lane, address arithmetic and softmax per 16 tokens took more issue slots than the
+// products: int8 rows came at 0.69 of the copy bandwidth.)
 //
 // Both products run on m16n8k16 with the long index on the 16-row side and the group's heads on the
 // 8-column side, as in the bounded cache's decode kernel:
@@ -27,12 +30,12 @@
 //                into the probabilities, relative to the largest scale met so far and times 2^14, in two
 //                parts; outputs are rescaled when that largest one grows, as they are for the maximum.
 #include "paged_internal.cuh"
+#include "sm100_ptx.cuh"
 
 namespace {
 
 using namespace buzz_paged_dev;
 
-constexpr int kTile = 16;
 constexpr int kHeads = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -52,21 +55,31 @@ __host__ __device__ constexpr int part_floats(int group, int d) { return group *
 template <typename T, typename C, int D>
 struct Plan {
   static constexpr bool kHalf = C::kScaled;            // fp16 operands
-  static constexpr int kWarps = C::kSize == 4 ? 4 : C::kSize == 2 ? 8 : 16;
-  static constexpr int kThreads = kWarps * 32;
   static constexpr int kRow = D * C::kSize;            // bytes of a row
+  static constexpr int kTok = buzz_paged_tile_tokens(kRow);
+  static constexpr int kSub = kTok / 16;               // 16-row parts of a tile
+  static constexpr int kWarps = kRow >= 256 ? 4 : 8;   // consumers: three stages of them fill 192 KB
+  static constexpr int kThreads = kWarps * 32 + 32;
+  static constexpr int kBox = buzz_paged_box_bytes(kRow);
+  static constexpr int kBoxes = kRow / kBox;
   static constexpr int kChunks = kRow / 16;            // 16-byte chunks of a row
   static constexpr int kE = 16 / C::kSize;             // elements of a chunk
-  static constexpr int kStage = 2 * kTile * kRow + (C::kScaled ? 2 * kTile * 4 : 0);
-  static constexpr int kSlots = 4;                     // outputs that warps leave for the merge at a time
-  static constexpr int kFit = (204 * 1024) / (kStage * kWarps);
+  static constexpr int kTileBytes = kTok * kRow;       // of K, and of V
+  static constexpr int kFit = (192 * 1024) / (2 * kTileBytes * kWarps);
   static constexpr int kStages = kFit > 6 ? 6 : kFit;
+  static constexpr int kRing = kWarps * kStages;       // tiles of the whole ring
+  static constexpr int kSlots = 4;                     // outputs that warps leave for the merge at a time
   static constexpr int kQ = sizeof(T) == 2 ? 1 : kHalf ? 2 : 3;    // parts of a query, of a probability, of a cached value
   static constexpr int kP = kHalf || sizeof(T) == 2 ? 2 : 3;
   static constexpr int kC = C::kSize == 4 ? 3 : 1;
   static_assert(kStages >= 2, "a ring holds two tiles at least");
+  static_assert(kBox == 128 || kBox == 64, "swizzles of 128 and 64 bytes");
+  // shared memory, from a multiple of 1024: ring | scales | barriers and row counts | merge
+  static constexpr int kScales = kRing * 2 * kTileBytes;
+  static constexpr int kBars = kScales + (C::kScaled ? kRing * 2 * kTok * 4 : 0);
+  static constexpr int kMerge = kBars + kRing * (8 + 8 + 4) + 16 - kRing * 20 % 16;
   static size_t smem(int group) {
-    return (size_t)kWarps * kStages * kStage + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads);
+    return 1024 + (size_t)kMerge + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads);
   }
 };
 
@@ -92,14 +105,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// 16 bytes global -> shared, or zeros where `on` is false (nothing is read then)
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // Two fp32 numbers as kN pairs of bf16 (or fp16) whose sums they are, to 8 (or 11) bits a part.
 template <int kN, bool kHalf>
 __device__ __forceinline__ void split(float a, float b, uint32_t (&w)[kN]) {
@@ -155,13 +160,6 @@ __device__ __forceinline__ void chunk_to_words(const uint4& u, uint32_t (&w)[kC]
   }
 }
 
-// Chunk positions are permuted per row so that the lanes of a 128-byte shared-memory wavefront meet
-// different banks: for K those are two neighbouring rows' four chunks, for V two chunks of rows 0, 2, 4, 6.
-template <int kChunks>
-__device__ __forceinline__ int swizzle_k(int row) { return kChunks >= 8 ? (row & 1) << 2 : 0; }
-template <int kChunks>
-__device__ __forceinline__ int swizzle_v(int row) { return kChunks >= 8 ? ((row >> 1) & 3) << 1 : (row >> 1) & 3; }
-
 // A place on the line of work.
 struct Place {
   int b, h, unit;       // sequence, KV head, unit within (b, h)
@@ -169,50 +167,68 @@ struct Place {
   bool bad;
 };
 
+template <int kTok>
 __device__ __forceinline__ int tiles_of(const DecodeArgs& a, const PagedView& w, int len) {
-  if (!a.selected) return (len + kTile - 1) / kTile;
+  if (!a.selected) return (len + kTok - 1) / kTok;
   const int pages = (len + (1 << w.page_log2) - 1) >> w.page_log2;
-  return min(pages, a.selected_stride) << (w.page_log2 - 4);
+  return ((min(pages, a.selected_stride) << w.page_log2) + kTok - 1) / kTok;
 }
-template <int kWarps>
+template <typename L>
 __device__ __forceinline__ void load_sequence(const DecodeArgs& a, const PagedView& w, Place& p) {
   const int len = a.lens[p.b];
   p.bad = len < 0 || len > a.max_len;
   p.len = p.bad ? 0 : len;
-  p.tiles = tiles_of(a, w, p.len);
-  p.units = max(1, (p.tiles + kWarps - 1) / kWarps);
+  p.tiles = tiles_of<L::kTok>(a, w, p.len);
+  p.units = max(1, (p.tiles + L::kWarps - 1) / L::kWarps);
 }
-template <int kWarps>
-__device__ __forceinline__ void advance(const DecodeArgs& a, const PagedView& w, Place& p) {
-  if (++p.unit < p.units) return;
-  p.unit = 0;
-  if (++p.h < w.kv_heads) return;
-  p.h = 0;
-  if (++p.b < a.batch) load_sequence<kWarps>(a, w, p);
+// `n` units on; past the last sequence p.b is batch
+template <typename L>
+__device__ __forceinline__ void advance(const DecodeArgs& a, const PagedView& w, Place& p, int n) {
+  while (n >= p.units - p.unit) {
+    n -= p.units - p.unit;
+    p.unit = 0;
+    if (++p.h == w.kv_heads) {
+      p.h = 0;
+      if (++p.b >= a.batch) return;
+      load_sequence<L>(a, w, p);
+    }
+  }
+  p.unit += n;
 }
+
+__device__ __forceinline__ void consumers_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
 template <typename T, typename C, int D>
 __global__ void __launch_bounds__(Plan<T, C, D>::kThreads, 1)
-paged_decode_kernel(const PagedView w, const DecodeArgs a) {
-  begin();
+paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using L = Plan<T, C, D>;
   constexpr int kWarps = L::kWarps, kThreads = L::kThreads, kChunks = L::kChunks, kE = L::kE, kStages = L::kStages;
-  constexpr int kSlots = L::kSlots;
+  constexpr int kTok = L::kTok, kSub = L::kSub, kBox = L::kBox, kBoxes = L::kBoxes, kSlots = L::kSlots;
   constexpr bool kHalf = L::kHalf;
   constexpr int kMK = kE / 4;                    // products per chunk of K
   constexpr int kKL = kChunks / 4;               // chunks per lane and key row
   constexpr int kVJ = kChunks >= 8 ? kChunks / 8 : 1;
   constexpr int kVE = D / 8 / kVJ;               // elements per lane, value row and j
-  constexpr int kOut = D / 16;                   // products per tile of V
+  constexpr int kOut = D / 16;                   // products per 16 rows of V
 
-  extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ long long warp_sum[kWarps];
-  __shared__ int found[2];
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, g = lane / 4, t = lane & 3;
-  unsigned char* ring = smem + (size_t)warp * kStages * L::kStage;
-  float* obuf = reinterpret_cast<float*>(smem + (size_t)kWarps * kStages * L::kStage);   // [slots][group][D]
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + (-(uint32_t)__cvta_generic_to_shared(smem_raw) & 1023u);
+  float* scales = reinterpret_cast<float*>(smem + L::kScales);                   // [ring][2][kTok]
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);                 // [warps][stages]
+  uint64_t* empty = full + L::kRing;
+  uint32_t* counts = reinterpret_cast<uint32_t*>(empty + L::kRing);              // valid rows of each 16-row part, a byte each
+  float* obuf = reinterpret_cast<float*>(smem + L::kMerge);                      // [slots][group][D]
   float* wm = obuf + kSlots * a.group * D;       // [warps][8] maxima, then sums
   float* wl = wm + kWarps * kHeads;
+  __shared__ long long warp_sum[kThreads / 32];
+  __shared__ int found[2];
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
+  for (int i = tid; i < L::kRing; i += kThreads) {
+    sm100::mbar_init(full + i, 1);
+    sm100::mbar_init(empty + i, 1);
+  }
+  sm100::fence_barrier_init();
+  begin();
 
   // ---- the line of work, and this block's stretch of it ----------------------------------------
   long long mine = 0;
@@ -221,7 +237,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
   for (int b = b_lo; b < b_hi; ++b) {
     Place p;
     p.b = b;
-    load_sequence<kWarps>(a, w, p);
+    load_sequence<L>(a, w, p);
     mine += p.units;
     if (p.bad && blockIdx.x == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, b, a.lens[b]);
   }
@@ -235,7 +251,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
   __syncthreads();
   long long before = 0, total = 0;
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
+  for (int i = 0; i < kThreads / 32; ++i) {
     if (i < warp) before += warp_sum[i];
     total += warp_sum[i];
   }
@@ -253,7 +269,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
       int b = b_lo;
       for (;; ++b) {
         p.b = b;
-        load_sequence<kWarps>(a, w, p);
+        load_sequence<L>(a, w, p);
         const long long here = (long long)p.units * w.kv_heads;
         if (u_begin < ex + here) break;
         ex += here;
@@ -265,74 +281,111 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
   __syncthreads();
   Place cur;
   cur.b = found[0];
-  load_sequence<kWarps>(a, w, cur);
+  load_sequence<L>(a, w, cur);
   cur.h = found[1] / cur.units;
   cur.unit = found[1] - cur.h * cur.units;
+  const int n_units = (int)(u_end - u_begin);
 
-  // ---- the ring: one tile per unit and warp ------------------------------------------------------
-  Place ahead = cur;
-  long long u_ahead = u_begin;
-  const uint32_t ring32 = (uint32_t)__cvta_generic_to_shared(ring);
-  uint32_t rows_left = 0;                        // valid rows of the tiles in the ring, five bits a stage
-  auto fetch = [&](int stage) {
-    int rows = 0;
-    if (u_ahead < u_end) {
-      const int tile = ahead.unit * kWarps + warp;
-      if (tile < ahead.tiles) {
-        const int sub = w.page_log2 - 4;         // log2 of the tiles of a page
-        int lp = tile >> sub;
-        if (a.selected) lp = a.selected[((int64_t)ahead.b * w.kv_heads + ahead.h) * a.selected_stride + lp];
-        const int pages = (ahead.len + (1 << w.page_log2) - 1) >> w.page_log2;
+  if (warp == kWarps) {
+    // ---- the fetching warp: lane i serves consumer i % kWarps, of each batch's unit i / kWarps ------
+    constexpr int kUnits = 32 / kWarps;          // units of a batch
+    const int to = lane % kWarps, my = lane / kWarps;
+    const int P = 1 << w.page_log2, box_rows = min(kTok, P);
+    const int parts = kTok / box_rows;           // pages of a tile: 1, or 2 of 16 tokens
+    struct Found { int row[2]; int rows; };      // first rows of the tile's pages (-1: none), valid rows of its 16-row parts
+    auto look_up = [&](const Place& p, bool on) {
+      Found f;
+      f.rows = 0;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        f.row[x] = -1;
+        if (!on || x >= parts) continue;
+        const int tile = p.unit * kWarps + to;
+        const int64_t token = (int64_t)tile * kTok + x * box_rows;       // of the pages to attend to, one after the other
+        int lp = (int)(token >> w.page_log2);
+        const int slot = (int)token & (P - 1);
+        const int pages = (p.len + P - 1) >> w.page_log2;
+        if (lp >= (a.selected ? min(pages, a.selected_stride) : pages)) continue;
+        if (a.selected) lp = a.selected[((int64_t)p.b * w.kv_heads + p.h) * a.selected_stride + lp];
         int page = -1;
-        if (lp >= 0 && lp < pages) page = a.table[(int64_t)ahead.b * a.table_stride + lp];
+        if (lp >= 0 && lp < pages) page = a.table[(int64_t)p.b * a.table_stride + lp];
         if (page < 0 || page >= w.pages) {
-          if (lane == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, ahead.b, lp);
-        } else {
-          const int slot = (tile & ((1 << sub) - 1)) * kTile;
-          rows = min(kTile, max(0, ahead.len - ((lp << w.page_log2) + slot)));
-          if (rows > 0) {
-            const size_t row0 = ((((size_t)page * w.kv_heads + ahead.h) << w.page_log2) + slot);
-            const char* ks = w.k + row0 * L::kRow;
-            const char* vs = w.v + row0 * L::kRow;
-            const uint32_t kd = ring32 + stage * L::kStage, vd = kd + kTile * L::kRow;
+          buzz_set_status(w.status, BUZZ_ERR_INVALID, p.b, lp);
+          continue;
+        }
+        const int valid = min(box_rows, p.len - (lp * P + slot));
+        if (valid <= 0) continue;
+        f.row[x] = ((page * w.kv_heads + p.h) << w.page_log2) + slot;
+        if (kSub == 1 || parts == 2) f.rows |= valid << (8 * x);
+        else f.rows = min(valid, 16) | (max(valid - 16, 0) << 8);
+      }
+      return f;
+    };
+    Place p = cur;
+    if (my > 0) advance<L>(a, w, p, my);
+    Found f = look_up(p, my < n_units);
+    bool alive = true;
+    for (int u0 = 0; u0 < n_units && alive; u0 += kUnits) {
+      if (u0 + my < n_units && p.unit == 0 && to == 0) {                 // the next consumers' query is fetched towards L2
+        const char* q = static_cast<const char*>(a.q) + ((size_t)p.b * w.kv_heads + p.h) * a.group * D * sizeof(T);
+        for (int i = 0; i < a.group * D * (int)sizeof(T); i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
+      }
+      const bool more = u0 + kUnits + my < n_units;
+      if (more) advance<L>(a, w, p, kUnits);
+      const Found next = look_up(p, more);
+#pragma unroll 1
+      for (int k = 0; k < kUnits && u0 + k < n_units; ++k) {
+        bool ok = true;
+        if (my == k) {
+          const int u = u0 + k, stage = u % kStages, turn = u / kStages, at = to * kStages + stage;
+          if (turn > 0) ok = sm100::mbar_wait(empty + at, (turn - 1) & 1);
+          if (ok) {
+            unsigned char* kt = smem + (size_t)at * 2 * L::kTileBytes;
+            unsigned char* vt = kt + L::kTileBytes;
+            counts[at] = f.rows;
+            const int boxes = (f.row[0] >= 0) + (f.row[1] >= 0);
+            if (boxes == 0) {
+              sm100::mbar_arrive(full + at);
+            } else {
+              sm100::mbar_expect_tx(full + at, boxes * (2 * box_rows * L::kRow + (C::kScaled ? 2 * box_rows * 4 : 0)));
 #pragma unroll
-            for (int i = 0; i < kTile * kChunks / 32; ++i) {
-              const int x = i * 32 + lane, r = x / kChunks, c = x % kChunks;
-              copy16(kd + r * L::kRow + ((c ^ swizzle_k<kChunks>(r)) * 16), ks + x * 16, r < rows);
-            }
+              for (int x = 0; x < 2; ++x) {
+                if (f.row[x] < 0) continue;
 #pragma unroll
-            for (int i = 0; i < kTile * kChunks / 32; ++i) {
-              const int x = i * 32 + lane, r = x / kChunks, c = x % kChunks;
-              copy16(vd + r * L::kRow + ((c ^ swizzle_v<kChunks>(r)) * 16), vs + x * 16, r < rows);
-            }
-            if constexpr (C::kScaled) {
-              if (lane < 8) {
-                const float* src = (lane < 4 ? w.k_scale : w.v_scale) + row0 + (lane & 3) * 4;
-                copy16(kd + 2 * kTile * L::kRow + lane * 16, src, true);     // whole tiles of scales exist; unused ones are masked
+                for (int i = 0; i < kBoxes; ++i) {
+                  sm100::tma_load_2d(kt + i * (kTok * kBox) + x * 16 * kBox, &k_map, i * kBox, w.row0 + f.row[x], full + at);
+                  sm100::tma_load_2d(vt + i * (kTok * kBox) + x * 16 * kBox, &v_map, i * kBox, w.row0 + f.row[x], full + at);
+                }
+                if constexpr (C::kScaled) {
+                  float* sc = scales + (size_t)at * 2 * kTok + x * 16;
+                  sm100::bulk_load_1d(sc, w.k_scale + f.row[x], box_rows * 4, full + at);
+                  sm100::bulk_load_1d(sc + kTok, w.v_scale + f.row[x], box_rows * 4, full + at);
+                }
               }
             }
           }
         }
+        alive = __all_sync(0xffffffffu, alive && ok);
+        if (!alive) {                            // a consumer that never came back: its own wait runs out as well
+          if (lane == 0) buzz_set_status(w.status, BUZZ_ERR_TIMEOUT, cur.b, u0);
+          break;
+        }
       }
-      ++u_ahead;
-      if (u_ahead < u_end) advance<kWarps>(a, w, ahead);
+      f = next;
     }
-    copy_commit();
-    rows_left = (rows_left & ~(31u << (5 * stage))) | ((uint32_t)rows << (5 * stage));
-  };
-#pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) fetch(s);
+    return;
+  }
 
+  // ---- consumers -----------------------------------------------------------------------------------
+  const int g = lane / 4, t = lane & 3;
   float oc[kOut][4], m[2], l[2];
   float q_unit[2] = {1.f, 1.f}, v_ref = 0.f, v_unit = 0.f;   // 8-bit caches: 2^-e of a head's query, largest value scale, 2^14 over it
-
   uint32_t qf[L::kQ][kKL * kMK][2];
-  int stage = 0;
   bool first_part = cur.unit == 0;               // the present (sequence, KV head) was begun by this block
-  bool begin = true;
-  for (long long u = u_begin; u < u_end; ++u) {
-    if (begin) {
-      begin = false;
+  bool start = true, alive = true;
+  for (int u = 0; u < n_units; ++u) {
+    if (start) {
+      start = false;
       m[0] = m[1] = -INFINITY;
       l[0] = l[1] = 0.f;
 #pragma unroll
@@ -373,41 +426,71 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
           for (int c = 0; c < L::kQ; ++c) qf[c][i][x] = s[c];
         }
     }
-    copy_wait<kStages - 2>();
-    __syncwarp();
-    fetch(stage == 0 ? kStages - 1 : stage - 1);   // the stage that the round before this one has read
-    const int rows = (rows_left >> (5 * stage)) & 31;
+    const int stage = u % kStages, at = warp * kStages + stage;
+    const bool came = sm100::mbar_wait(full + at, (u / kStages) & 1, alive ? sm100::kWaitPolls : 64);
+    if (!__all_sync(0xffffffffu, came)) {
+      if (alive && lane == 0) buzz_set_status(w.status, BUZZ_ERR_TIMEOUT, cur.b, u);
+      alive = false;
+    }
+    const uint32_t rows = alive ? counts[at] : 0;
     if (rows > 0) {
-      const unsigned char* kt = ring + stage * L::kStage;
-      const unsigned char* vt = kt + kTile * L::kRow;
-      // S^T = K Q^T
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      const unsigned char* kt = smem + (size_t)at * 2 * L::kTileBytes;
+      unsigned char* vt = smem + (size_t)at * 2 * L::kTileBytes + L::kTileBytes;
+      if (rows != (kSub == 2 ? 0x1010u : 0x10u)) {                       // what a page holds behind the sequence may be anything
+        for (int r = 0; r < kTok; ++r) {
+          if ((r & 15) < (int)(rows >> (8 * (r / 16)) & 255)) continue;
 #pragma unroll
-      for (int i = 0; i < kKL; ++i) {
-        uint32_t lo[L::kC][kE / 2], hi[L::kC][kE / 2];
-        const int c = (4 * i + t) ^ swizzle_k<kChunks>(g);             // rows g and g + 8 have one parity
-        chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + g * L::kRow + c * 16), lo);
-        chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(kt + (g + 8) * L::kRow + c * 16), hi);
-#pragma unroll
-        for (int mm = 0; mm < kMK; ++mm)
-#pragma unroll
-          for (int kc = L::kC - 1; kc >= 0; --kc)
-#pragma unroll
-            for (int qc = L::kQ - 1; qc >= 0; --qc) {
-              if (kc + qc > 2) continue;
-              const uint32_t fr[4] = {lo[kc][2 * mm], hi[kc][2 * mm], lo[kc][2 * mm + 1], hi[kc][2 * mm + 1]};
-              mma<kHalf>(s, fr, qf[qc][i * kMK + mm][0], qf[qc][i * kMK + mm][1]);
-            }
+          for (int i = 0; i < kBoxes; ++i)
+            if (lane < kBox / 4) *reinterpret_cast<uint32_t*>(vt + i * (kTok * kBox) + r * kBox + lane * 4) = 0;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the next copy into this stage
+        __syncwarp();
       }
-      // s[0], s[1]: key g, heads 2t, 2t+1; s[2], s[3]: key g + 8
-      float scale = a.scale_log2, vs0 = 1.f, vs1 = 1.f, ks0 = 1.f, ks1 = 1.f, grow = 1.f;
+      // S^T = K Q^T
+      float s[kSub][4];
+#pragma unroll
+      for (int b = 0; b < kSub; ++b) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[b][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kKL; ++i) {
+          uint32_t lo[L::kC][kE / 2], hi[L::kC][kE / 2];
+          // rows g and g + 8 of the part have one swizzle
+          const int c = kBox == 128 ? ((4 * (i & 1) + t) ^ g) : (t ^ (g >> 1 & 3));
+          const unsigned char* src = kt + (kBox == 128 ? i / 2 : 0) * (kTok * kBox) + (b * 16 + g) * kBox + c * 16;
+          chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(src), lo);
+          chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(src + 8 * kBox), hi);
+#pragma unroll
+          for (int mm = 0; mm < kMK; ++mm)
+#pragma unroll
+            for (int kc = L::kC - 1; kc >= 0; --kc)
+#pragma unroll
+              for (int qc = L::kQ - 1; qc >= 0; --qc) {
+                if (kc + qc > 2) continue;
+                const uint32_t fr[4] = {lo[kc][2 * mm], hi[kc][2 * mm], lo[kc][2 * mm + 1], hi[kc][2 * mm + 1]};
+                mma<kHalf>(s[b], fr, qf[qc][i * kMK + mm][0], qf[qc][i * kMK + mm][1]);
+              }
+        }
+      }
+      // s[b][0], s[b][1]: key g of part b, heads 2t, 2t+1; s[b][2], s[b][3]: key g + 8
+      float scale = a.scale_log2, grow = 1.f, ks[kSub][2], vs[kSub][2];
+      bool live[kSub][2];
       if (a.logn) scale *= __logf((float)cur.len) * (1.0f / 6.2383246250395077f);
+      float big = 0.f;
+#pragma unroll
+      for (int b = 0; b < kSub; ++b)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          live[b][y] = g + 8 * y < (int)(rows >> (8 * b) & 255);
+          ks[b][y] = vs[b][y] = 1.f;
+          if constexpr (C::kScaled) {
+            const float* sc = scales + (size_t)at * 2 * kTok + b * 16 + g + 8 * y;
+            ks[b][y] = sc[0];
+            vs[b][y] = live[b][y] ? sc[kTok] : 0.f;
+            big = fmaxf(big, vs[b][y]);
+          }
+        }
       if constexpr (C::kScaled) {
-        const float* sc = reinterpret_cast<const float*>(vt + kTile * L::kRow);
-        ks0 = sc[g]; ks1 = sc[g + 8]; vs0 = sc[kTile + g]; vs1 = sc[kTile + g + 8];
-        if (g >= rows) vs0 = 0.f;
-        if (g + 8 >= rows) vs1 = 0.f;
-        float big = fmaxf(vs0, vs1);
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
         if (big > v_ref) {                                             // the same in all lanes
@@ -415,24 +498,37 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
           v_ref = big;
           v_unit = 16384.f / big;
         }
-        vs0 *= v_unit;
-        vs1 *= v_unit;
       }
-      float p[4], f[2];
+      float f[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        p[e] = g < rows ? s[e] * (ks0 * (scale * q_unit[e])) : -INFINITY;
-        p[2 + e] = g + 8 < rows ? s[2 + e] * (ks1 * (scale * q_unit[e])) : -INFINITY;
-        float top = fmaxf(p[e], p[2 + e]);
+        const float unit = scale * q_unit[e];
+        float top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < kSub; ++b)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float& x = s[b][2 * y + e];
+            x = live[b][y] ? x * (C::kScaled ? ks[b][y] * unit : unit) : -INFINITY;
+            top = fmaxf(top, x);
+          }
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
         const float next = fmaxf(m[e], top);
         const float base = next == -INFINITY ? 0.f : next;             // keys of logit -inf weigh nothing
         f[e] = exp2f(m[e] - base);
         m[e] = next;
-        p[e] = exp2f(p[e] - base);
-        p[2 + e] = exp2f(p[2 + e] - base);
-        l[e] = l[e] * f[e] + (p[e] + p[2 + e]);
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < kSub; ++b)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float& x = s[b][2 * y + e];
+            x = exp2f(x - base);
+            sum += x;
+            if constexpr (C::kScaled) x *= vs[b][y] * v_unit;
+          }
+        l[e] = l[e] * f[e] + sum;
         f[e] *= grow;
       }
       if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
@@ -441,66 +537,70 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) oc[i][e] *= f[e & 1];
       }
-      // P^T fragments: the probabilities (times the values' scales), transposed from keys x heads
-      uint32_t pa[L::kP], pb[L::kP], f0[L::kP], f1[L::kP];
-      split<L::kP, kHalf>(p[0] * vs0, p[1] * vs0, pa);
-      split<L::kP, kHalf>(p[2] * vs1, p[3] * vs1, pb);
 #pragma unroll
-      for (int c = 0; c < L::kP; ++c) { f0[c] = transpose8x8(pa[c]); f1[c] = transpose8x8(pb[c]); }
-      // O^T += V^T P^T
-      if constexpr (kHalf) {
-        // rows are paired byte by byte before they are widened: half the permutes
-        constexpr int kWords = D / 32;               // words of four dims per lane and row
-        uint32_t vb[4][kWords];
+      for (int b = 0; b < kSub; ++b) {
+        // P^T fragments: the probabilities (times the values' scales), transposed from keys x heads
+        uint32_t pa[L::kP], pb[L::kP], f0[L::kP], f1[L::kP];
+        split<L::kP, kHalf>(s[b][0], s[b][1], pa);
+        split<L::kP, kHalf>(s[b][2], s[b][3], pb);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int r = 2 * t + (x & 1) + (x >> 1) * 8;
-          if constexpr (kChunks >= 8) {
-            const uint4 u = *reinterpret_cast<const uint4*>(vt + r * L::kRow + (g ^ swizzle_v<kChunks>(r)) * 16);
-            vb[x][0] = u.x; vb[x][1] = u.y; vb[x][2] = u.z; vb[x][3] = u.w;
-          } else {                                   // 64 dims: eight bytes of a chunk
-            const uint2 u = *reinterpret_cast<const uint2*>(vt + r * L::kRow + ((g >> 1) ^ swizzle_v<kChunks>(r)) * 16 + (g & 1) * 8);
-            vb[x][0] = u.x; vb[x][1] = u.y;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < kWords; ++i)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            uint32_t fr[4];
-            codes_to_half<C>(__byte_perm(vb[0][i], vb[1][i], k ? 0x7362 : 0x5140), fr[0], fr[1]);
-            codes_to_half<C>(__byte_perm(vb[2][i], vb[3][i], k ? 0x7362 : 0x5140), fr[2], fr[3]);
-#pragma unroll
-            for (int pc = L::kP - 1; pc >= 0; --pc) mma_f16(oc[2 * i + k], fr, f0[pc], f1[pc]);
-          }
-      } else {
-#pragma unroll
-        for (int j = 0; j < kVJ; ++j) {
-          uint32_t vw[4][L::kC][kVE / 2];
+        for (int c = 0; c < L::kP; ++c) { f0[c] = transpose8x8(pa[c]); f1[c] = transpose8x8(pb[c]); }
+        // O^T += V^T P^T; value rows 2t, 2t+1, 2t+8, 2t+9 of the part
+        const unsigned char* vr = vt + (b * 16 + 2 * t) * kBox;
+        if constexpr (kHalf) {
+          // rows are paired byte by byte before they are widened: half the permutes
+          constexpr int kWords = D / 32;             // words of four dims per lane and row
+          uint32_t vb[4][kWords];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const int r = 2 * t + (x & 1) + (x >> 1) * 8;
-            const int c = (g + 8 * j) ^ swizzle_v<kChunks>(r);
-            chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(vt + r * L::kRow + c * 16), vw[x]);
+            const unsigned char* src = vr + ((x & 1) + (x >> 1) * 8) * kBox;
+            if constexpr (kBox == 128) {
+              const uint4 u4 = *reinterpret_cast<const uint4*>(src + ((g ^ (2 * t + (x & 1))) * 16));
+              vb[x][0] = u4.x; vb[x][1] = u4.y; vb[x][2] = u4.z; vb[x][3] = u4.w;
+            } else {                                 // 64 dims: eight bytes of a chunk
+              const uint2 u2 = *reinterpret_cast<const uint2*>(src + ((g >> 1) ^ t) * 16 + (g & 1) * 8);
+              vb[x][0] = u2.x; vb[x][1] = u2.y;
+            }
           }
 #pragma unroll
-          for (int i = 0; i < kVE / 2; ++i)
+          for (int i = 0; i < kWords; ++i)
 #pragma unroll
-            for (int vc = L::kC - 1; vc >= 0; --vc) {
-              const uint32_t fr[4] = {__byte_perm(vw[0][vc][i], vw[1][vc][i], 0x5410), __byte_perm(vw[0][vc][i], vw[1][vc][i], 0x7632),
-                                      __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x5410), __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x7632)};
+            for (int k = 0; k < 2; ++k) {
+              uint32_t fr[4];
+              codes_to_half<C>(__byte_perm(vb[0][i], vb[1][i], k ? 0x7362 : 0x5140), fr[0], fr[1]);
+              codes_to_half<C>(__byte_perm(vb[2][i], vb[3][i], k ? 0x7362 : 0x5140), fr[2], fr[3]);
 #pragma unroll
-              for (int pc = L::kP - 1; pc >= 0; --pc)
-                if (vc + pc <= 2) mma_bf16(oc[j * (kVE / 2) + i], fr, f0[pc], f1[pc]);
+              for (int pc = L::kP - 1; pc >= 0; --pc) mma_f16(oc[2 * i + k], fr, f0[pc], f1[pc]);
             }
+        } else {
+#pragma unroll
+          for (int j = 0; j < kVJ; ++j) {
+            uint32_t vw[4][L::kC][kVE / 2];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const unsigned char* src = vr + j * (kTok * kBox) + ((x & 1) + (x >> 1) * 8) * kBox + ((g ^ (2 * t + (x & 1))) * 16);
+              chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(src), vw[x]);
+            }
+#pragma unroll
+            for (int i = 0; i < kVE / 2; ++i)
+#pragma unroll
+              for (int vc = L::kC - 1; vc >= 0; --vc) {
+                const uint32_t fr[4] = {__byte_perm(vw[0][vc][i], vw[1][vc][i], 0x5410), __byte_perm(vw[0][vc][i], vw[1][vc][i], 0x7632),
+                                        __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x5410), __byte_perm(vw[2][vc][i], vw[3][vc][i], 0x7632)};
+#pragma unroll
+                for (int pc = L::kP - 1; pc >= 0; --pc)
+                  if (vc + pc <= 2) mma_bf16(oc[j * (kVE / 2) + i], fr, f0[pc], f1[pc]);
+              }
+          }
         }
       }
     }
-    stage = stage + 1 == kStages ? 0 : stage + 1;
+    __syncwarp();
+    if (lane == 0) sm100::mbar_arrive(empty + at);
 
     // ---- end of this (sequence, KV head), or of the block's stretch of it -----------------------
     const bool complete = cur.unit + 1 == cur.units;
-    if (complete || u + 1 == u_end) {
+    if (complete || u + 1 == n_units) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -509,7 +609,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) { wm[warp * kHeads + 2 * t + e] = m[e]; wl[warp * kHeads + 2 * t + e] = l[e]; }
       }
-      __syncthreads();
+      consumers_sync(kWarps * 32);
       float top[2], f[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -535,48 +635,47 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a) {
               *o = v;
             }
         }
-        __syncthreads();
+        consumers_sync(kWarps * 32);
       }
       const bool whole = complete && first_part;
       const size_t head0 = ((size_t)cur.b * w.kv_heads + cur.h) * a.group;
       float* part = a.part + ((size_t)blockIdx.x * 2 + (first_part ? 1 : 0)) * part_floats(a.group, D);
-      for (int x = tid; x < a.group * D; x += kThreads) {
+      for (int x = tid; x < a.group * D; x += kWarps * 32) {
         const int hd = x / D;
-        float big = -INFINITY, sum = 0.f, o = 0.f;
+        float most = -INFINITY, sum = 0.f, o = 0.f;
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) big = fmaxf(big, wm[i * kHeads + hd]);
+        for (int i = 0; i < kWarps; ++i) most = fmaxf(most, wm[i * kHeads + hd]);
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) {
           const float mi = wm[i * kHeads + hd];
-          sum += mi == -INFINITY ? 0.f : wl[i * kHeads + hd] * exp2f(mi - big);
+          sum += mi == -INFINITY ? 0.f : wl[i * kHeads + hd] * exp2f(mi - most);
         }
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) o += obuf[i * a.group * D + x];
         if (whole) {
           if (!cur.bad) {
             static_cast<T*>(a.out)[head0 * D + x] = (T)(sum == 0.f ? 0.f : o / sum);
-            if (a.lse && x % D == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (big + log2f(sum)) * 0.69314718055994531f;
+            if (a.lse && x % D == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (most + log2f(sum)) * 0.69314718055994531f;
           }
         } else {
           part[x] = o;
-          if (x % D == 0) { part[a.group * D + hd] = big; part[a.group * D + kHeads + hd] = sum; }
+          if (x % D == 0) { part[a.group * D + hd] = most; part[a.group * D + kHeads + hd] = sum; }
         }
       }
-      if (!complete && tid == 0) {
+      if (u + 1 == n_units && tid == 0) {
         // the join of an instance is described where the instance begins
-        if (first_part) {
-          const long long end = u + (cur.units - cur.unit);                      // its first unit past the end
-          a.desc[blockIdx.x] = make_int4((int)(cur.b * (long long)w.kv_heads + cur.h), (int)((end * n - 1) / U), 0, 0);
-        } else {
-          a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        int4 d = make_int4(-1, 0, 0, 0);
+        if (!complete && first_part) {
+          const long long end = u_begin + u + (cur.units - cur.unit);                    // its first unit past the end
+          d = make_int4((int)(cur.b * (long long)w.kv_heads + cur.h), (int)((end * n - 1) / U), 0, 0);
         }
+        a.desc[blockIdx.x] = d;
       }
-      if (complete && u + 1 == u_end && tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
-      __syncthreads();
-      begin = true;
+      consumers_sync(kWarps * 32);
+      start = true;
       first_part = true;
     }
-    if (u + 1 < u_end) advance<kWarps>(a, w, cur);
+    if (u + 1 < n_units) advance<L>(a, w, cur, 1);
   }
 }
 
@@ -643,28 +742,25 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
   else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
-int blocks_for(const buzz_paged* c, int batch, long long max_tiles, int warps) {
-  const long long units = (long long)batch * c->sh.kv_heads * ((max_tiles + warps - 1) / warps > 0 ? (max_tiles + warps - 1) / warps : 1);
-  return (int)(units < c->sm_count ? units : c->sm_count);
-}
-
 template <typename T, typename C, int D>
 cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) {
   using L = Plan<T, C, D>;
-  long long tiles = ((long long)a.max_len + kTile - 1) / kTile;
+  long long tokens = a.max_len;
   if (a.selected) {
-    const long long most = (long long)a.selected_stride << (c->page_log2 - 4);
-    const long long round = ((tiles >> (c->page_log2 - 4)) + 1) << (c->page_log2 - 4);
-    tiles = most < round ? most : round;
+    const long long most = (long long)a.selected_stride << c->page_log2, round = ((tokens >> c->page_log2) + 1) << c->page_log2;
+    tokens = most < round ? most : round;
   }
-  const int n = blocks_for(c, a.batch, tiles, L::kWarps);
+  const long long units = (tokens + L::kTok * L::kWarps - 1) / (L::kTok * L::kWarps);          // of a (sequence, KV head), at most
+  const long long all = (long long)a.batch * c->sh.kv_heads * (units > 0 ? units : 1);
+  const int n = (int)(all < c->sm_count ? all : c->sm_count);
   const size_t smem = L::smem(c->group);
   static BuzzSmemOptIn opt_in;
   if (cudaError_t e = opt_in.ensure(paged_decode_kernel<T, C, D>, smem); e != cudaSuccess) return e;
-  if (cudaError_t e = buzz_launch_chained(paged_decode_kernel<T, C, D>, dim3(n), L::kThreads, smem, stream, c->view(layer), a); e != cudaSuccess)
+  if (cudaError_t e = buzz_launch_chained(paged_decode_kernel<T, C, D>, dim3(n), L::kThreads, smem, stream, c->view(layer), a, c->k_map, c->v_map);
+      e != cudaSuccess)
     return e;
   c->launches += 1;
-  if (tiles <= L::kWarps) return cudaSuccess;      // one unit per (sequence, KV head): nothing is ever split
+  if (units <= 1) return cudaSuccess;              // nothing is ever split
   cudaError_t e = buzz_launch_chained(paged_join_kernel<T, D>, dim3(n), (unsigned)kJoinThreads, sizeof(float) * c->group * n, stream, a);
   if (e == cudaSuccess) c->launches += 1;
   return e;

@@ -2,6 +2,7 @@
 // cache's element types and what the kernels compute with.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
@@ -18,6 +19,7 @@ struct PagedView {
   float* v_scale;
   char* bounds;        // null where the pool has none
   int32_t* status;
+  int row0;            // the layer's first row (page, KV head, slot) in the tensor maps over all layers
   int pages;           // pages of the pool
   int kv_heads;
   int page_log2;       // log2(page_tokens)
@@ -31,6 +33,7 @@ struct buzz_paged {
   int sm_count;        // multiprocessors of the device that was current at buzz_paged_create
   size_t esize, csize; // bytes per element of `dtype` and of the cache
   long long launches;
+  CUtensorMap k_map, v_map;   // [rows of all layers][bytes of a row], boxes of one tile's rows (paged_decode.cu)
   PagedView view(int layer) const {
     const size_t rows = (size_t)layer * sh.pages * sh.kv_heads * sh.page_tokens;
     PagedView w;
@@ -40,12 +43,22 @@ struct buzz_paged {
     w.v_scale = buf.v_scale ? buf.v_scale + rows : nullptr;
     w.bounds = buf.bounds ? static_cast<char*>(buf.bounds) + (size_t)layer * sh.pages * sh.kv_heads * 2 * sh.head_dim * esize : nullptr;
     w.status = buf.status;
+    w.row0 = (int)rows;
     w.pages = sh.pages;
     w.kv_heads = sh.kv_heads;
     w.page_log2 = page_log2;
     return w;
   }
 };
+
+// Geometry of the tiles that attention reads: tokens of a tile, and the box that one tensor copy brings.
+// A box is at most 128 bytes wide (the widest swizzle) and lies within one page.
+constexpr int buzz_paged_tile_tokens(int row_bytes) { return row_bytes >= 512 ? 16 : 32; }
+constexpr int buzz_paged_box_bytes(int row_bytes) { return row_bytes < 128 ? row_bytes : 128; }
+inline int buzz_paged_box_rows(int row_bytes, int page_tokens) {
+  const int t = buzz_paged_tile_tokens(row_bytes);
+  return t < page_tokens ? t : page_tokens;
+}
 
 // Element types of a cache as template tags.
 struct CacheF32 { static constexpr int kSize = 4; static constexpr bool kScaled = false; };
