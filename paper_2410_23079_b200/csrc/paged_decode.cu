@@ -29,6 +29,8 @@
 //                stay exact down to 2^-28 of it; fp32 queries are two parts). The values' row scales go
 //                into the probabilities, relative to the largest scale met so far and times 2^14, in two
 //                parts; outputs are rescaled when that largest one grows, as they are for the maximum.
+#include <type_traits>
+
 #include "paged_internal.cuh"
 #include "sm100_ptx.cuh"
 
@@ -38,6 +40,8 @@ using namespace buzz_paged_dev;
 
 constexpr int kHeads = 8;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 6.f;        // log2 of the largest probability before the maximum in use is raised
+constexpr float kUnit = 256.f;       // 8-bit caches: weight of a probability of 1 at the largest value scale; times 2^kSlack and 2, below 2^16
 
 struct DecodeArgs {
   const void* q;
@@ -72,6 +76,7 @@ struct Plan {
   static constexpr int kQ = sizeof(T) == 2 ? 1 : kHalf ? 2 : 3;    // parts of a query, of a probability, of a cached value
   static constexpr int kP = kHalf || sizeof(T) == 2 ? 2 : 3;
   static constexpr int kC = C::kSize == 4 ? 3 : 1;
+  static constexpr bool kOffset = sizeof(T) == 2 && C::kScaled && std::is_same<C, CacheI8>::value;   // keys of int8 keep their offset of 1152
   static_assert(kStages >= 2, "a ring holds two tiles at least");
   static_assert(kBox == 128 || kBox == 64, "swizzles of 128 and 64 bytes");
   // shared memory, from a multiple of 1024: ring | scales | barriers and row counts | merge
@@ -84,13 +89,13 @@ struct Plan {
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -102,7 +107,7 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 // Two fp32 numbers as kN pairs of bf16 (or fp16) whose sums they are, to 8 (or 11) bits a part.
@@ -122,7 +127,7 @@ __device__ __forceinline__ void split(float a, float b, uint32_t (&w)[kN]) {
 }
 
 // Four 8-bit codes of a word as two pairs of fp16, exact. int8: a byte offset by 128 below the exponent of 2^10.
-template <typename C>
+template <typename C, bool kOffset>
 __device__ __forceinline__ void codes_to_half(uint32_t x, uint32_t& lo, uint32_t& hi) {
   if constexpr (C::kTop == 448.f) {
     const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffffu), __NV_E4M3);
@@ -132,6 +137,7 @@ __device__ __forceinline__ void codes_to_half(uint32_t x, uint32_t& lo, uint32_t
   } else {
     const uint32_t o = x ^ 0x80808080u;
     const uint32_t a = __byte_perm(o, 0x64646464u, 0x4140), b = __byte_perm(o, 0x64646464u, 0x4342);
+    if constexpr (kOffset) { lo = a; hi = b; return; }
     const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));     // 1152
     const __half2 ha = __hsub2(*reinterpret_cast<const __half2*>(&a), off), hb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
     lo = *reinterpret_cast<const uint32_t*>(&ha);
@@ -140,7 +146,7 @@ __device__ __forceinline__ void codes_to_half(uint32_t x, uint32_t& lo, uint32_t
 }
 
 // A 16-byte chunk of the cache as kE / 2 words of two operands each, kC parts.
-template <typename C, int kC, int kE>
+template <typename C, int kC, int kE, bool kOffset>
 __device__ __forceinline__ void chunk_to_words(const uint4& u, uint32_t (&w)[kC][kE / 2]) {
   const uint32_t x[4] = {u.x, u.y, u.z, u.w};
   if constexpr (C::kSize == 2) {
@@ -148,7 +154,7 @@ __device__ __forceinline__ void chunk_to_words(const uint4& u, uint32_t (&w)[kC]
     for (int i = 0; i < 4; ++i) w[0][i] = x[i];
   } else if constexpr (C::kSize == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) codes_to_half<C>(x[i], w[0][2 * i], w[0][2 * i + 1]);
+    for (int i = 0; i < 4; ++i) codes_to_half<C, kOffset>(x[i], w[0][2 * i], w[0][2 * i + 1]);
   } else {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -164,6 +170,7 @@ __device__ __forceinline__ void chunk_to_words(const uint4& u, uint32_t (&w)[kC]
 struct Place {
   int b, h, unit;       // sequence, KV head, unit within (b, h)
   int len, tiles, units;
+  int next;             // the next sequence's length, loaded ahead of its use
   bool bad;
 };
 
@@ -174,8 +181,7 @@ __device__ __forceinline__ int tiles_of(const DecodeArgs& a, const PagedView& w,
   return ((min(pages, a.selected_stride) << w.page_log2) + kTok - 1) / kTok;
 }
 template <typename L>
-__device__ __forceinline__ void load_sequence(const DecodeArgs& a, const PagedView& w, Place& p) {
-  const int len = a.lens[p.b];
+__device__ __forceinline__ void set_sequence(const DecodeArgs& a, const PagedView& w, Place& p, int len) {
   p.bad = len < 0 || len > a.max_len;
   p.len = p.bad ? 0 : len;
   p.tiles = tiles_of<L::kTok>(a, w, p.len);
@@ -190,7 +196,8 @@ __device__ __forceinline__ void advance(const DecodeArgs& a, const PagedView& w,
     if (++p.h == w.kv_heads) {
       p.h = 0;
       if (++p.b >= a.batch) return;
-      load_sequence<L>(a, w, p);
+      set_sequence<L>(a, w, p, p.next);
+      if (p.b + 1 < a.batch) p.next = a.lens[p.b + 1];
     }
   }
   p.unit += n;
@@ -236,8 +243,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   const int b_lo = min(tid * per, a.batch), b_hi = min(b_lo + per, a.batch);
   for (int b = b_lo; b < b_hi; ++b) {
     Place p;
-    p.b = b;
-    load_sequence<L>(a, w, p);
+    set_sequence<L>(a, w, p, a.lens[b]);
     mine += p.units;
     if (p.bad && blockIdx.x == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, b, a.lens[b]);
   }
@@ -268,8 +274,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
       Place p;
       int b = b_lo;
       for (;; ++b) {
-        p.b = b;
-        load_sequence<L>(a, w, p);
+        set_sequence<L>(a, w, p, a.lens[b]);
         const long long here = (long long)p.units * w.kv_heads;
         if (u_begin < ex + here) break;
         ex += here;
@@ -281,7 +286,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   __syncthreads();
   Place cur;
   cur.b = found[0];
-  load_sequence<L>(a, w, cur);
+  set_sequence<L>(a, w, cur, a.lens[cur.b]);
+  cur.next = cur.b + 1 < a.batch ? a.lens[cur.b + 1] : 0;
   cur.h = found[1] / cur.units;
   cur.unit = found[1] - cur.h * cur.units;
   const int n_units = (int)(u_end - u_begin);
@@ -292,47 +298,70 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
     const int to = lane % kWarps, my = lane / kWarps;
     const int P = 1 << w.page_log2, box_rows = min(kTok, P);
     const int parts = kTok / box_rows;           // pages of a tile: 1, or 2 of 16 tokens
-    struct Found { int row[2]; int rows; };      // first rows of the tile's pages (-1: none), valid rows of its 16-row parts
-    auto look_up = [&](const Place& p, bool on) {
-      Found f;
-      f.rows = 0;
+    // A look-up takes three steps a batch apart, so that the loads of one are back when the next wants
+    // them: the logical page (where pages are selected, from memory), the physical page, the rows.
+    struct Look { int index[2], logical[2], page[2], len, h, b; };
+    auto look_logical = [&](Look& f, const Place& p, bool on) {
+      f.len = on ? p.len : 0;
+      f.h = p.h;
+      f.b = p.b;
+      const int pages = (f.len + P - 1) >> w.page_log2;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        f.row[x] = -1;
-        if (!on || x >= parts) continue;
-        const int tile = p.unit * kWarps + to;
-        const int64_t token = (int64_t)tile * kTok + x * box_rows;       // of the pages to attend to, one after the other
-        int lp = (int)(token >> w.page_log2);
-        const int slot = (int)token & (P - 1);
-        const int pages = (p.len + P - 1) >> w.page_log2;
-        if (lp >= (a.selected ? min(pages, a.selected_stride) : pages)) continue;
-        if (a.selected) lp = a.selected[((int64_t)p.b * w.kv_heads + p.h) * a.selected_stride + lp];
-        int page = -1;
-        if (lp >= 0 && lp < pages) page = a.table[(int64_t)p.b * a.table_stride + lp];
-        if (page < 0 || page >= w.pages) {
-          buzz_set_status(w.status, BUZZ_ERR_INVALID, p.b, lp);
+        const int64_t token = (int64_t)(p.unit * kWarps + to) * kTok + x * box_rows;      // of the pages to attend to, one after the other
+        f.index[x] = x < parts && (token >> w.page_log2) < (a.selected ? min(pages, a.selected_stride) : pages) ? (int)token : -1;
+        f.logical[x] = (int)(token >> w.page_log2);
+        if (a.selected && f.index[x] >= 0)
+          f.logical[x] = a.selected[((int64_t)p.b * w.kv_heads + p.h) * a.selected_stride + f.logical[x]];
+      }
+    };
+    auto look_page = [&](Look& f) {
+      const int pages = (f.len + P - 1) >> w.page_log2;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        f.page[x] = -1;
+        if (f.index[x] >= 0 && f.logical[x] >= 0 && f.logical[x] < pages) f.page[x] = a.table[(int64_t)f.b * a.table_stride + f.logical[x]];
+      }
+    };
+    // first rows of the tile's pages (-1: none), and the valid rows of its 16-row parts, a byte each
+    auto look_rows = [&](const Look& f, int (&row)[2]) {
+      int rows = 0;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        row[x] = -1;
+        if (f.index[x] < 0) continue;
+        if (f.page[x] < 0 || f.page[x] >= w.pages) {
+          buzz_set_status(w.status, BUZZ_ERR_INVALID, f.b, f.logical[x]);
           continue;
         }
-        const int valid = min(box_rows, p.len - (lp * P + slot));
+        const int slot = f.index[x] & (P - 1), valid = min(box_rows, f.len - (f.logical[x] * P + slot));
         if (valid <= 0) continue;
-        f.row[x] = ((page * w.kv_heads + p.h) << w.page_log2) + slot;
-        if (kSub == 1 || parts == 2) f.rows |= valid << (8 * x);
-        else f.rows = min(valid, 16) | (max(valid - 16, 0) << 8);
+        row[x] = ((f.page[x] * w.kv_heads + f.h) << w.page_log2) + slot;
+        if (kSub == 1 || parts == 2) rows |= valid << (8 * x);
+        else rows = min(valid, 16) | (max(valid - 16, 0) << 8);
       }
-      return f;
+      return rows;
     };
     Place p = cur;
     if (my > 0) advance<L>(a, w, p, my);
-    Found f = look_up(p, my < n_units);
+    Look now, next;
+    look_logical(now, p, my < n_units);
     bool alive = true;
+    if (kUnits + my < n_units) advance<L>(a, w, p, kUnits);
+    look_logical(next, p, kUnits + my < n_units);
+    look_page(now);
     for (int u0 = 0; u0 < n_units && alive; u0 += kUnits) {
-      if (u0 + my < n_units && p.unit == 0 && to == 0) {                 // the next consumers' query is fetched towards L2
+      look_page(next);
+      Look later;
+      const bool more = u0 + 2 * kUnits + my < n_units;
+      if (more) advance<L>(a, w, p, kUnits);
+      look_logical(later, p, more);
+      if (more && p.unit == 0 && to == 0) {                              // the consumers' next query is fetched towards L2
         const char* q = static_cast<const char*>(a.q) + ((size_t)p.b * w.kv_heads + p.h) * a.group * D * sizeof(T);
         for (int i = 0; i < a.group * D * (int)sizeof(T); i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
       }
-      const bool more = u0 + kUnits + my < n_units;
-      if (more) advance<L>(a, w, p, kUnits);
-      const Found next = look_up(p, more);
+      int row[2];
+      const int rows = look_rows(now, row);
 #pragma unroll 1
       for (int k = 0; k < kUnits && u0 + k < n_units; ++k) {
         bool ok = true;
@@ -342,24 +371,24 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
           if (ok) {
             unsigned char* kt = smem + (size_t)at * 2 * L::kTileBytes;
             unsigned char* vt = kt + L::kTileBytes;
-            counts[at] = f.rows;
-            const int boxes = (f.row[0] >= 0) + (f.row[1] >= 0);
+            counts[at] = rows;
+            const int boxes = (row[0] >= 0) + (row[1] >= 0);
             if (boxes == 0) {
               sm100::mbar_arrive(full + at);
             } else {
               sm100::mbar_expect_tx(full + at, boxes * (2 * box_rows * L::kRow + (C::kScaled ? 2 * box_rows * 4 : 0)));
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
-                if (f.row[x] < 0) continue;
+                if (row[x] < 0) continue;
 #pragma unroll
                 for (int i = 0; i < kBoxes; ++i) {
-                  sm100::tma_load_2d(kt + i * (kTok * kBox) + x * 16 * kBox, &k_map, i * kBox, w.row0 + f.row[x], full + at);
-                  sm100::tma_load_2d(vt + i * (kTok * kBox) + x * 16 * kBox, &v_map, i * kBox, w.row0 + f.row[x], full + at);
+                  sm100::tma_load_2d(kt + i * (kTok * kBox) + x * 16 * kBox, &k_map, i * kBox, w.row0 + row[x], full + at);
+                  sm100::tma_load_2d(vt + i * (kTok * kBox) + x * 16 * kBox, &v_map, i * kBox, w.row0 + row[x], full + at);
                 }
                 if constexpr (C::kScaled) {
                   float* sc = scales + (size_t)at * 2 * kTok + x * 16;
-                  sm100::bulk_load_1d(sc, w.k_scale + f.row[x], box_rows * 4, full + at);
-                  sm100::bulk_load_1d(sc + kTok, w.v_scale + f.row[x], box_rows * 4, full + at);
+                  sm100::bulk_load_1d(sc, w.k_scale + row[x], box_rows * 4, full + at);
+                  sm100::bulk_load_1d(sc + kTok, w.v_scale + row[x], box_rows * 4, full + at);
                 }
               }
             }
@@ -371,7 +400,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
           break;
         }
       }
-      f = next;
+      now = next;
+      next = later;
     }
     return;
   }
@@ -381,6 +411,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   float oc[kOut][4], m[2], l[2];
   float q_unit[2] = {1.f, 1.f}, v_ref = 0.f, v_unit = 0.f;   // 8-bit caches: 2^-e of a head's query, largest value scale, 2^14 over it
   uint32_t qf[L::kQ][kKL * kMK][2];
+  float s_off[2] = {0.f, 0.f};
   bool first_part = cur.unit == 0;               // the present (sequence, KV head) was begun by this block
   bool start = true, alive = true;
   for (int u = 0; u < n_units; ++u) {
@@ -425,6 +456,14 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
 #pragma unroll
           for (int c = 0; c < L::kQ; ++c) qf[c][i][x] = s[c];
         }
+      if constexpr (L::kOffset) {                // what the offset of the codes adds to every logit, negated
+        const uint32_t minus[4] = {0xE480E480u, 0xE480E480u, 0xE480E480u, 0xE480E480u};        // -1152
+        float off[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kKL * kMK; ++i) mma_f16(off, minus, qf[0][i][0], qf[0][i][1]);
+        s_off[0] = off[0];
+        s_off[1] = off[1];
+      }
     }
     const int stage = u % kStages, at = warp * kStages + stage;
     const bool came = sm100::mbar_wait(full + at, (u / kStages) & 1, alive ? sm100::kWaitPolls : 64);
@@ -450,16 +489,17 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
       float s[kSub][4];
 #pragma unroll
       for (int b = 0; b < kSub; ++b) {
+        float s2[2][4];                              // two chains of products: one alone waits for itself
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[b][e] = 0.f;
+        for (int e = 0; e < 4; ++e) { s2[0][e] = s_off[e & 1]; s2[1][e] = 0.f; }
 #pragma unroll
         for (int i = 0; i < kKL; ++i) {
           uint32_t lo[L::kC][kE / 2], hi[L::kC][kE / 2];
           // rows g and g + 8 of the part have one swizzle
           const int c = kBox == 128 ? ((4 * (i & 1) + t) ^ g) : (t ^ (g >> 1 & 3));
           const unsigned char* src = kt + (kBox == 128 ? i / 2 : 0) * (kTok * kBox) + (b * 16 + g) * kBox + c * 16;
-          chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(src), lo);
-          chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(src + 8 * kBox), hi);
+          chunk_to_words<C, L::kC, kE, L::kOffset>(*reinterpret_cast<const uint4*>(src), lo);
+          chunk_to_words<C, L::kC, kE, L::kOffset>(*reinterpret_cast<const uint4*>(src + 8 * kBox), hi);
 #pragma unroll
           for (int mm = 0; mm < kMK; ++mm)
 #pragma unroll
@@ -468,9 +508,11 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
               for (int qc = L::kQ - 1; qc >= 0; --qc) {
                 if (kc + qc > 2) continue;
                 const uint32_t fr[4] = {lo[kc][2 * mm], hi[kc][2 * mm], lo[kc][2 * mm + 1], hi[kc][2 * mm + 1]};
-                mma<kHalf>(s[b], fr, qf[qc][i * kMK + mm][0], qf[qc][i * kMK + mm][1]);
+                mma<kHalf>(s2[(i * kMK + mm) & 1], fr, qf[qc][i * kMK + mm][0], qf[qc][i * kMK + mm][1]);
               }
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[b][e] = s2[0][e] + s2[1][e];
       }
       // s[b][0], s[b][1]: key g of part b, heads 2t, 2t+1; s[b][2], s[b][3]: key g + 8
       float scale = a.scale_log2, grow = 1.f, ks[kSub][2], vs[kSub][2];
@@ -490,52 +532,63 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
             big = fmaxf(big, vs[b][y]);
           }
         }
-      if constexpr (C::kScaled) {
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
-        if (big > v_ref) {                                             // the same in all lanes
-          grow = v_ref / big;
-          v_ref = big;
-          v_unit = 16384.f / big;
-        }
-      }
-      float f[2];
+      // The maximum in use (and the largest value scale) is raised only when a logit exceeds it by more than
+      // kSlack, or a scale twofold: probabilities are then 2^kSlack at most, and a tile needs no exchange
+      // between lanes. A vote decides for the warp.
+      bool raise = big > 2.f * v_ref;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float unit = scale * q_unit[e];
-        float top = -INFINITY;
+        const float unit = scale * q_unit[e], limit = m[e] + kSlack;
 #pragma unroll
         for (int b = 0; b < kSub; ++b)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             float& x = s[b][2 * y + e];
             x = live[b][y] ? x * (C::kScaled ? ks[b][y] * unit : unit) : -INFINITY;
-            top = fmaxf(top, x);
+            raise |= x > limit;
           }
+      }
+      if (__any_sync(0xffffffffu, raise)) {
+        if constexpr (C::kScaled) {
 #pragma unroll
-        for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-        const float next = fmaxf(m[e], top);
-        const float base = next == -INFINITY ? 0.f : next;             // keys of logit -inf weigh nothing
-        f[e] = exp2f(m[e] - base);
-        m[e] = next;
-        float sum = 0.f;
+          for (int off = 4; off < 32; off <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, off));
+          if (big > v_ref) {                                           // the same in all lanes
+            grow = v_ref / big;
+            v_ref = big;
+            v_unit = kUnit / big;
+          }
+        }
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int b = 0; b < kSub; ++b) top = fmaxf(top, fmaxf(s[b][e], s[b][2 + e]));
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+          const float next = fmaxf(m[e], top);
+          f[e] = next == -INFINITY ? 1.f : exp2f(m[e] - next);
+          m[e] = next;
+          l[e] *= f[e];
+          f[e] *= grow;
+        }
+#pragma unroll
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) oc[i][e] *= f[e & 1];
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float base = m[e] == -INFINITY ? 0.f : m[e];             // keys of logit -inf weigh nothing
 #pragma unroll
         for (int b = 0; b < kSub; ++b)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             float& x = s[b][2 * y + e];
             x = exp2f(x - base);
-            sum += x;
+            l[e] += x;
             if constexpr (C::kScaled) x *= vs[b][y] * v_unit;
           }
-        l[e] = l[e] * f[e] + sum;
-        f[e] *= grow;
-      }
-      if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
-#pragma unroll
-        for (int i = 0; i < kOut; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) oc[i][e] *= f[e & 1];
       }
 #pragma unroll
       for (int b = 0; b < kSub; ++b) {
@@ -567,8 +620,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               uint32_t fr[4];
-              codes_to_half<C>(__byte_perm(vb[0][i], vb[1][i], k ? 0x7362 : 0x5140), fr[0], fr[1]);
-              codes_to_half<C>(__byte_perm(vb[2][i], vb[3][i], k ? 0x7362 : 0x5140), fr[2], fr[3]);
+              codes_to_half<C, false>(__byte_perm(vb[0][i], vb[1][i], k ? 0x7362 : 0x5140), fr[0], fr[1]);
+              codes_to_half<C, false>(__byte_perm(vb[2][i], vb[3][i], k ? 0x7362 : 0x5140), fr[2], fr[3]);
 #pragma unroll
               for (int pc = L::kP - 1; pc >= 0; --pc) mma_f16(oc[2 * i + k], fr, f0[pc], f1[pc]);
             }
@@ -579,7 +632,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const unsigned char* src = vr + j * (kTok * kBox) + ((x & 1) + (x >> 1) * 8) * kBox + ((g ^ (2 * t + (x & 1))) * 16);
-              chunk_to_words<C, L::kC, kE>(*reinterpret_cast<const uint4*>(src), vw[x]);
+              chunk_to_words<C, L::kC, kE, false>(*reinterpret_cast<const uint4*>(src), vw[x]);
             }
 #pragma unroll
             for (int i = 0; i < kVE / 2; ++i)
@@ -617,7 +670,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) top[e] = fmaxf(top[e], wm[i * kHeads + 2 * t + e]);
         f[e] = m[e] == -INFINITY ? 0.f : exp2f(m[e] - top[e]);
-        if constexpr (kHalf) f[e] *= v_ref * (1.f / 16384.f);
+        if constexpr (kHalf) f[e] *= v_ref * (1.f / kUnit);
       }
 #pragma unroll
       for (int round = 0; round < kWarps / kSlots; ++round) {            // in turn, so that the merge fits beside the ring
