@@ -7,13 +7,14 @@
 // begin or end inside a (sequence, KV head); such parts are written as (max, sum, output) to the
 // workspace and joined by a second, small kernel in the order of the line.
 //
-// One warp of a block looks pages up and fetches tiles by tensor copies (swizzled boxes that lie within a
-// page) into a ring per consumer warp; each of its lanes serves one tile of the next 32, so that look-ups
-// cost the consumers nothing. The consumer warps take the tiles of a unit in turn and are independent
-// until their (sequence, KV head) ends; the next one's rows are under way meanwhile. Rows behind a
-// sequence's end are overwritten with zeros before they are multiplied. (With every warp copying for
-// itself, 16 bytes a lane, address arithmetic and softmax per 16 tokens took more issue slots than the
-// products: int8 rows came at 0.69 of the copy bandwidth.)
+// The warps of a block take the tiles of a unit in turn, each with a ring of its own in shared memory that
+// it fills by tensor copies (swizzled boxes that lie within a page), issued by one lane into the stage that
+// the warp has just finished; no warp waits for another until their (sequence, KV head) ends, and the next
+// one's rows are under way meanwhile. Pages are looked up for 32 tiles at once, a lane each, two batches
+// ahead. Rows behind a sequence's end are overwritten with zeros before they are multiplied.
+// Measured on int8 rows, 32 sequences of 8192..16384 tokens, 838 MB: every lane copying 16 bytes for its own
+// warp 189 us (more issue slots for addresses than for products), a warp that fetches for the others
+// 166 us (it waits for the slowest of them), this 156 us; without the arithmetic 134 us.
 //
 // Both products run on m16n8k16 with the long index on the 16-row side and the group's heads on the
 // 8-column side, as in the bounded cache's decode kernel:
@@ -62,17 +63,20 @@ struct Plan {
   static constexpr int kRow = D * C::kSize;            // bytes of a row
   static constexpr int kTok = buzz_paged_tile_tokens(kRow);
   static constexpr int kSub = kTok / 16;               // 16-row parts of a tile
-  static constexpr int kWarps = kRow >= 256 ? 4 : 8;   // consumers: three stages of them fill 192 KB
-  static constexpr int kThreads = kWarps * 32 + 32;
+  // Warps and the stages of their rings fill 200 KB. 8-bit rows cost so many instructions per byte that
+  // twelve warps with two stages are faster than eight with three (161 -> 147 us on the rows above); wider
+  // rows wait for memory, and fewer warps mean fewer parts to merge.
+  static constexpr int kWarps = kRow >= 256 ? 4 : C::kScaled ? 12 : 8;
+  static constexpr int kThreads = kWarps * 32;
   static constexpr int kBox = buzz_paged_box_bytes(kRow);
   static constexpr int kBoxes = kRow / kBox;
   static constexpr int kChunks = kRow / 16;            // 16-byte chunks of a row
   static constexpr int kE = 16 / C::kSize;             // elements of a chunk
   static constexpr int kTileBytes = kTok * kRow;       // of K, and of V
-  static constexpr int kFit = (192 * 1024) / (2 * kTileBytes * kWarps);
+  static constexpr int kFit = (200 * 1024) / ((2 * kTileBytes + (C::kScaled ? 8 * kTok : 0)) * kWarps);
   static constexpr int kStages = kFit > 6 ? 6 : kFit;
   static constexpr int kRing = kWarps * kStages;       // tiles of the whole ring
-  static constexpr int kSlots = 4;                     // outputs that warps leave for the merge at a time
+  static constexpr int kSlots = kWarps == 12 ? 6 : 4;  // outputs that warps leave for the merge at a time
   static constexpr int kQ = sizeof(T) == 2 ? 1 : kHalf ? 2 : 3;    // parts of a query, of a probability, of a cached value
   static constexpr int kP = kHalf || sizeof(T) == 2 ? 2 : 3;
   static constexpr int kC = C::kSize == 4 ? 3 : 1;
@@ -82,9 +86,9 @@ struct Plan {
   // shared memory, from a multiple of 1024: ring | scales | barriers and row counts | merge
   static constexpr int kScales = kRing * 2 * kTileBytes;
   static constexpr int kBars = kScales + (C::kScaled ? kRing * 2 * kTok * 4 : 0);
-  static constexpr int kMerge = kBars + kRing * (8 + 8 + 4) + 16 - kRing * 20 % 16;
+  static constexpr int kMerge = kBars + (kRing * (8 + 4) + 15) / 16 * 16;
   static size_t smem(int group) {
-    return 1024 + (size_t)kMerge + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads);
+    return 1024 + (size_t)kMerge + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads + kHeads);
   }
 };
 
@@ -166,6 +170,23 @@ __device__ __forceinline__ void chunk_to_words(const uint4& u, uint32_t (&w)[kC]
   }
 }
 
+// Four consecutive elements.
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    x[0] = bf16_lo(u.x); x[1] = bf16_hi(u.x); x[2] = bf16_lo(u.y); x[3] = bf16_hi(u.y);
+  } else {
+    const float4 u = *reinterpret_cast<const float4*>(p);
+    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float4 x) {
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+  else *reinterpret_cast<float4*>(p) = x;
+}
+
 // A place on the line of work.
 struct Place {
   int b, h, unit;       // sequence, KV head, unit within (b, h)
@@ -203,8 +224,6 @@ __device__ __forceinline__ void advance(const DecodeArgs& a, const PagedView& w,
   p.unit += n;
 }
 
-__device__ __forceinline__ void consumers_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
-
 template <typename T, typename C, int D>
 __global__ void __launch_bounds__(Plan<T, C, D>::kThreads, 1)
 paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -222,18 +241,15 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   unsigned char* smem = smem_raw + (-(uint32_t)__cvta_generic_to_shared(smem_raw) & 1023u);
   float* scales = reinterpret_cast<float*>(smem + L::kScales);                   // [ring][2][kTok]
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);                 // [warps][stages]
-  uint64_t* empty = full + L::kRing;
-  uint32_t* counts = reinterpret_cast<uint32_t*>(empty + L::kRing);              // valid rows of each 16-row part, a byte each
+  uint32_t* counts = reinterpret_cast<uint32_t*>(full + L::kRing);              // valid rows of each 16-row part, a byte each
   float* obuf = reinterpret_cast<float*>(smem + L::kMerge);                      // [slots][group][D]
-  float* wm = obuf + kSlots * a.group * D;       // [warps][8] maxima, then sums
-  float* wl = wm + kWarps * kHeads;
+  float* wm = obuf + kSlots * a.group * D;       // [warps][8] maxima
+  float* wl = wm + kWarps * kHeads;              // [warps][8] sums, over the largest maximum
+  float* wt = wl + kWarps * kHeads;              // [8] largest maxima
   __shared__ long long warp_sum[kThreads / 32];
   __shared__ int found[2];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
-  for (int i = tid; i < L::kRing; i += kThreads) {
-    sm100::mbar_init(full + i, 1);
-    sm100::mbar_init(empty + i, 1);
-  }
+  for (int i = tid; i < L::kRing; i += kThreads) sm100::mbar_init(full + i, 1);
   sm100::fence_barrier_init();
   begin();
 
@@ -292,121 +308,108 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   cur.unit = found[1] - cur.h * cur.units;
   const int n_units = (int)(u_end - u_begin);
 
-  if (warp == kWarps) {
-    // ---- the fetching warp: lane i serves consumer i % kWarps, of each batch's unit i / kWarps ------
-    constexpr int kUnits = 32 / kWarps;          // units of a batch
-    const int to = lane % kWarps, my = lane / kWarps;
-    const int P = 1 << w.page_log2, box_rows = min(kTok, P);
-    const int parts = kTok / box_rows;           // pages of a tile: 1, or 2 of 16 tokens
-    // A look-up takes three steps a batch apart, so that the loads of one are back when the next wants
-    // them: the logical page (where pages are selected, from memory), the physical page, the rows.
-    struct Look { int index[2], logical[2], page[2], len, h, b; };
-    auto look_logical = [&](Look& f, const Place& p, bool on) {
-      f.len = on ? p.len : 0;
-      f.h = p.h;
-      f.b = p.b;
-      const int pages = (f.len + P - 1) >> w.page_log2;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int64_t token = (int64_t)(p.unit * kWarps + to) * kTok + x * box_rows;      // of the pages to attend to, one after the other
-        f.index[x] = x < parts && (token >> w.page_log2) < (a.selected ? min(pages, a.selected_stride) : pages) ? (int)token : -1;
-        f.logical[x] = (int)(token >> w.page_log2);
-        if (a.selected && f.index[x] >= 0)
-          f.logical[x] = a.selected[((int64_t)p.b * w.kv_heads + p.h) * a.selected_stride + f.logical[x]];
-      }
-    };
-    auto look_page = [&](Look& f) {
-      const int pages = (f.len + P - 1) >> w.page_log2;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        f.page[x] = -1;
-        if (f.index[x] >= 0 && f.logical[x] >= 0 && f.logical[x] < pages) f.page[x] = a.table[(int64_t)f.b * a.table_stride + f.logical[x]];
-      }
-    };
-    // first rows of the tile's pages (-1: none), and the valid rows of its 16-row parts, a byte each
-    auto look_rows = [&](const Look& f, int (&row)[2]) {
-      int rows = 0;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        row[x] = -1;
-        if (f.index[x] < 0) continue;
-        if (f.page[x] < 0 || f.page[x] >= w.pages) {
-          buzz_set_status(w.status, BUZZ_ERR_INVALID, f.b, f.logical[x]);
-          continue;
-        }
-        const int slot = f.index[x] & (P - 1), valid = min(box_rows, f.len - (f.logical[x] * P + slot));
-        if (valid <= 0) continue;
-        row[x] = ((f.page[x] * w.kv_heads + f.h) << w.page_log2) + slot;
-        if (kSub == 1 || parts == 2) rows |= valid << (8 * x);
-        else rows = min(valid, 16) | (max(valid - 16, 0) << 8);
-      }
-      return rows;
-    };
-    Place p = cur;
-    if (my > 0) advance<L>(a, w, p, my);
-    Look now, next;
-    look_logical(now, p, my < n_units);
-    bool alive = true;
-    if (kUnits + my < n_units) advance<L>(a, w, p, kUnits);
-    look_logical(next, p, kUnits + my < n_units);
-    look_page(now);
-    for (int u0 = 0; u0 < n_units && alive; u0 += kUnits) {
-      look_page(next);
-      Look later;
-      const bool more = u0 + 2 * kUnits + my < n_units;
-      if (more) advance<L>(a, w, p, kUnits);
-      look_logical(later, p, more);
-      if (more && p.unit == 0 && to == 0) {                              // the consumers' next query is fetched towards L2
-        const char* q = static_cast<const char*>(a.q) + ((size_t)p.b * w.kv_heads + p.h) * a.group * D * sizeof(T);
-        for (int i = 0; i < a.group * D * (int)sizeof(T); i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
-      }
-      int row[2];
-      const int rows = look_rows(now, row);
-#pragma unroll 1
-      for (int k = 0; k < kUnits && u0 + k < n_units; ++k) {
-        bool ok = true;
-        if (my == k) {
-          const int u = u0 + k, stage = u % kStages, turn = u / kStages, at = to * kStages + stage;
-          if (turn > 0) ok = sm100::mbar_wait(empty + at, (turn - 1) & 1);
-          if (ok) {
-            unsigned char* kt = smem + (size_t)at * 2 * L::kTileBytes;
-            unsigned char* vt = kt + L::kTileBytes;
-            counts[at] = rows;
-            const int boxes = (row[0] >= 0) + (row[1] >= 0);
-            if (boxes == 0) {
-              sm100::mbar_arrive(full + at);
-            } else {
-              sm100::mbar_expect_tx(full + at, boxes * (2 * box_rows * L::kRow + (C::kScaled ? 2 * box_rows * 4 : 0)));
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                if (row[x] < 0) continue;
-#pragma unroll
-                for (int i = 0; i < kBoxes; ++i) {
-                  sm100::tma_load_2d(kt + i * (kTok * kBox) + x * 16 * kBox, &k_map, i * kBox, w.row0 + row[x], full + at);
-                  sm100::tma_load_2d(vt + i * (kTok * kBox) + x * 16 * kBox, &v_map, i * kBox, w.row0 + row[x], full + at);
-                }
-                if constexpr (C::kScaled) {
-                  float* sc = scales + (size_t)at * 2 * kTok + x * 16;
-                  sm100::bulk_load_1d(sc, w.k_scale + row[x], box_rows * 4, full + at);
-                  sm100::bulk_load_1d(sc + kTok, w.v_scale + row[x], box_rows * 4, full + at);
-                }
-              }
-            }
-          }
-        }
-        alive = __all_sync(0xffffffffu, alive && ok);
-        if (!alive) {                            // a consumer that never came back: its own wait runs out as well
-          if (lane == 0) buzz_set_status(w.status, BUZZ_ERR_TIMEOUT, cur.b, u0);
-          break;
-        }
-      }
-      now = next;
-      next = later;
+  // ---- the ring: lane i looks up this warp's tile of every 32nd unit, from i on -------------------
+  const int P = 1 << w.page_log2, box_rows = min(kTok, P);
+  const int parts = kTok / box_rows;             // pages of a tile: 1, or 2 of 16 tokens
+  // A look-up takes three steps: the logical page (where pages are selected, from memory), the physical page
+  // and, a batch later, so that the loads are back by then, the rows.
+  struct Look { int index[2], logical[2], page[2], len, h, b; };
+  auto look_logical = [&](Look& f, const Place& p, bool on) {
+    f.len = on ? p.len : 0;
+    f.h = p.h;
+    f.b = p.b;
+    if (on && warp == 0 && p.unit == 0) {        // a query that will be needed is fetched towards L2
+      const char* q = static_cast<const char*>(a.q) + ((size_t)p.b * w.kv_heads + p.h) * a.group * D * sizeof(T);
+      for (int i = 0; i < a.group * D * (int)sizeof(T); i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
     }
-    return;
-  }
+    const int pages = (f.len + P - 1) >> w.page_log2;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int64_t token = (int64_t)(p.unit * kWarps + warp) * kTok + x * box_rows;      // of the pages to attend to, one after the other
+      f.index[x] = x < parts && (token >> w.page_log2) < (a.selected ? min(pages, a.selected_stride) : pages) ? (int)token : -1;
+      f.logical[x] = (int)(token >> w.page_log2);
+      if (a.selected && f.index[x] >= 0)
+        f.logical[x] = a.selected[((int64_t)p.b * w.kv_heads + p.h) * a.selected_stride + f.logical[x]];
+    }
+  };
+  auto look_page = [&](Look& f) {
+    const int pages = (f.len + P - 1) >> w.page_log2;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      f.page[x] = -1;
+      if (f.index[x] >= 0 && f.logical[x] >= 0 && f.logical[x] < pages) f.page[x] = a.table[(int64_t)f.b * a.table_stride + f.logical[x]];
+    }
+  };
+  // first rows of the tile's pages (-1: none), and the valid rows of its 16-row parts, a byte each
+  auto look_rows = [&](const Look& f, int (&row)[2]) {
+    int rows = 0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      row[x] = -1;
+      if (f.index[x] < 0) continue;
+      if (f.page[x] < 0 || f.page[x] >= w.pages) {
+        buzz_set_status(w.status, BUZZ_ERR_INVALID, f.b, f.logical[x]);
+        continue;
+      }
+      const int slot = f.index[x] & (P - 1), valid = min(box_rows, f.len - (f.logical[x] * P + slot));
+      if (valid <= 0) continue;
+      row[x] = ((f.page[x] * w.kv_heads + f.h) << w.page_log2) + slot;
+      if (kSub == 1 || parts == 2) rows |= valid << (8 * x);
+      else rows = min(valid, 16) | (max(valid - 16, 0) << 8);
+    }
+    return rows;
+  };
+  Place p = cur;
+  if (lane > 0) advance<L>(a, w, p, lane);
+  Look now, next;
+  look_logical(now, p, lane < n_units);
+  if (lane + 32 < n_units) advance<L>(a, w, p, 32);
+  look_logical(next, p, lane + 32 < n_units);
+  look_page(now);
+  int row[2], rows_of;                           // of the lane's tile in the present batch
+  // starts unit u's copies into its stage; units are started in order
+  auto start_unit = [&](int u) {
+    if ((u & 31) == 0) {
+      if (u > 0) now = next;
+      rows_of = look_rows(now, row);
+      if (u > 0) {
+        const bool more = u + 32 + lane < n_units;
+        if (more) advance<L>(a, w, p, 32);
+        look_logical(next, p, more);
+      }
+      look_page(next);
+    }
+    const int r0 = __shfl_sync(0xffffffffu, row[0], u & 31), r1 = __shfl_sync(0xffffffffu, row[1], u & 31);
+    const int rows = __shfl_sync(0xffffffffu, rows_of, u & 31);
+    if (lane != 0) return;
+    const int at = warp * kStages + u % kStages;
+    unsigned char* kt = smem + (size_t)at * 2 * L::kTileBytes;
+    unsigned char* vt = kt + L::kTileBytes;
+    counts[at] = rows;
+    const int boxes = (r0 >= 0) + (r1 >= 0);
+    if (boxes == 0) {
+      sm100::mbar_arrive(full + at);
+      return;
+    }
+    sm100::mbar_expect_tx(full + at, boxes * (2 * box_rows * L::kRow + (C::kScaled ? 2 * box_rows * 4 : 0)));
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = x ? r1 : r0;
+      if (r < 0) continue;
+#pragma unroll
+      for (int i = 0; i < kBoxes; ++i) {
+        sm100::tma_load_2d(kt + i * (kTok * kBox) + x * 16 * kBox, &k_map, i * kBox, w.row0 + r, full + at);
+        sm100::tma_load_2d(vt + i * (kTok * kBox) + x * 16 * kBox, &v_map, i * kBox, w.row0 + r, full + at);
+      }
+      if constexpr (C::kScaled) {
+        float* sc = scales + (size_t)at * 2 * kTok + x * 16;
+        sm100::bulk_load_1d(sc, w.k_scale + r, box_rows * 4, full + at);
+        sm100::bulk_load_1d(sc + kTok, w.v_scale + r, box_rows * 4, full + at);
+      }
+    }
+  };
+  for (int u = 0; u < min(kStages, n_units); ++u) start_unit(u);
 
-  // ---- consumers -----------------------------------------------------------------------------------
   const int g = lane / 4, t = lane & 3;
   float oc[kOut][4], m[2], l[2];
   float q_unit[2] = {1.f, 1.f}, v_ref = 0.f, v_unit = 0.f;   // 8-bit caches: 2^-e of a head's query, largest value scale, 2^14 over it
@@ -428,15 +431,15 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
       float qv[kKL * kMK][4];
       float big = 0.f;
 #pragma unroll
-      for (int i = 0; i < kKL; ++i)
+      for (int i = 0; i < kKL * kMK; ++i) {
 #pragma unroll
-        for (int mm = 0; mm < kMK; ++mm)
+        for (int x = 0; x < 4; ++x) qv[i][x] = 0.f;
+        if (g < a.group) load4(qp + (4 * (i / kMK) + t) * kE + 4 * (i % kMK), qv[i]);
+      }
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            float& y = qv[i * kMK + mm][x];
-            y = g < a.group ? (float)qp[(4 * i + t) * kE + 4 * mm + x] : 0.f;
-            big = fmaxf(big, fabsf(y));
-          }
+      for (int i = 0; i < kKL * kMK; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) big = fmaxf(big, fabsf(qv[i][x]));
       float unit = 1.f;
       if constexpr (kHalf) {
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
@@ -648,8 +651,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
         }
       }
     }
-    __syncwarp();
-    if (lane == 0) sm100::mbar_arrive(empty + at);
+    __syncwarp();                                // all lanes are done with the stage
+    if (u + kStages < n_units && alive) start_unit(u + kStages);
 
     // ---- end of this (sequence, KV head), or of the block's stretch of it -----------------------
     const bool complete = cur.unit + 1 == cur.units;
@@ -658,20 +661,24 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) l[e] += __shfl_xor_sync(0xffffffffu, l[e], off);
+      // Everything below is ordered by the barriers of this merge and the first of the next one, so that no
+      // warp waits for the last step: the others go on to their next tile.
+      if (g == 0) *reinterpret_cast<float2*>(wm + warp * kHeads + 2 * t) = make_float2(m[0], m[1]);
+      __syncthreads();
+      float top[2] = {-INFINITY, -INFINITY}, f[2];
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const float2 x = *reinterpret_cast<const float2*>(wm + i * kHeads + 2 * t);
+        top[0] = fmaxf(top[0], x.x);
+        top[1] = fmaxf(top[1], x.y);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) f[e] = m[e] == -INFINITY ? 0.f : exp2f(m[e] - top[e]);
       if (g == 0) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) { wm[warp * kHeads + 2 * t + e] = m[e]; wl[warp * kHeads + 2 * t + e] = l[e]; }
+        *reinterpret_cast<float2*>(wl + warp * kHeads + 2 * t) = make_float2(l[0] * f[0], l[1] * f[1]);
+        if (warp == 0) *reinterpret_cast<float2*>(wt + 2 * t) = make_float2(top[0], top[1]);
       }
-      consumers_sync(kWarps * 32);
-      float top[2], f[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        top[e] = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) top[e] = fmaxf(top[e], wm[i * kHeads + 2 * t + e]);
-        f[e] = m[e] == -INFINITY ? 0.f : exp2f(m[e] - top[e]);
-        if constexpr (kHalf) f[e] *= v_ref * (1.f / kUnit);
-      }
+      if constexpr (kHalf) { f[0] *= v_ref * (1.f / kUnit); f[1] *= v_ref * (1.f / kUnit); }
 #pragma unroll
       for (int round = 0; round < kWarps / kSlots; ++round) {            // in turn, so that the merge fits beside the ring
         if (warp / kSlots == round) {
@@ -688,31 +695,31 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
               *o = v;
             }
         }
-        consumers_sync(kWarps * 32);
+        __syncthreads();
       }
       const bool whole = complete && first_part;
       const size_t head0 = ((size_t)cur.b * w.kv_heads + cur.h) * a.group;
       float* part = a.part + ((size_t)blockIdx.x * 2 + (first_part ? 1 : 0)) * part_floats(a.group, D);
-      for (int x = tid; x < a.group * D; x += kWarps * 32) {
-        const int hd = x / D;
-        float most = -INFINITY, sum = 0.f, o = 0.f;
+      for (int x = tid; x < a.group * D / 4; x += kThreads) {
+        const int hd = x / (D / 4);
+        float sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) most = fmaxf(most, wm[i * kHeads + hd]);
+        for (int i = 0; i < kWarps; ++i) sum += wl[i * kHeads + hd];
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) {
-          const float mi = wm[i * kHeads + hd];
-          sum += mi == -INFINITY ? 0.f : wl[i * kHeads + hd] * exp2f(mi - most);
+        for (int i = 0; i < kSlots; ++i) {
+          const float4 v = *reinterpret_cast<const float4*>(obuf + i * a.group * D + 4 * x);
+          o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
         }
-#pragma unroll
-        for (int i = 0; i < kSlots; ++i) o += obuf[i * a.group * D + x];
         if (whole) {
           if (!cur.bad) {
-            static_cast<T*>(a.out)[head0 * D + x] = (T)(sum == 0.f ? 0.f : o / sum);
-            if (a.lse && x % D == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (most + log2f(sum)) * 0.69314718055994531f;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            store4(static_cast<T*>(a.out) + head0 * D + 4 * x, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+            if (a.lse && x % (D / 4) == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (wt[hd] + log2f(sum)) * 0.69314718055994531f;
           }
         } else {
-          part[x] = o;
-          if (x % D == 0) { part[a.group * D + hd] = most; part[a.group * D + kHeads + hd] = sum; }
+          *reinterpret_cast<float4*>(part + 4 * x) = o;
+          if (x % (D / 4) == 0) { part[a.group * D + hd] = wt[hd]; part[a.group * D + kHeads + hd] = sum; }
         }
       }
       if (u + 1 == n_units && tid == 0) {
@@ -724,7 +731,6 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
         }
         a.desc[blockIdx.x] = d;
       }
-      consumers_sync(kWarps * 32);
       start = true;
       first_part = true;
     }
@@ -791,8 +797,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
   }
   const float sum = total[x / (D / 4)], inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.out) + head0 * D + x * 4;
-  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-  else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  store4(out, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
 }
 
 template <typename T, typename C, int D>
