@@ -134,10 +134,7 @@ __device__ __forceinline__ void split(float a, float b, uint32_t (&w)[kN]) {
 template <typename C, bool kOffset>
 __device__ __forceinline__ void codes_to_half(uint32_t x, uint32_t& lo, uint32_t& hi) {
   if constexpr (C::kTop == 448.f) {
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffffu), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x >> 16), __NV_E4M3);
-    lo = a.x | ((uint32_t)a.y << 16);
-    hi = b.x | ((uint32_t)b.y << 16);
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(x));
   } else {
     const uint32_t o = x ^ 0x80808080u;
     const uint32_t a = __byte_perm(o, 0x64646464u, 0x4140), b = __byte_perm(o, 0x64646464u, 0x4342);
