@@ -9,8 +9,8 @@
 //
 // A warp takes a run of heads of ONE token, so that a lane's eight sines and cosines stay in registers
 // over all of them (read from shared memory per row they cost bank conflicts that took as long as the
-// traffic), and issues the loads of four rounds of rows before it uses the first. Few tokens are cut into
-// more runs, for the sake of more warps. Angles are formed in fp64 (a position of a million times a
+// traffic), and keeps the loads of four rounds of rows under way. Few tokens are cut into more runs, for
+// the sake of more warps. Angles are formed in fp64 (a position of a million times a
 // frequency near one leaves fp32 no digits after the point), reduced to half turns there, then sinpi and
 // cospi in fp32 (error below 1e-7); each lane forms some and the warp shares them.
 #include "paged_internal.cuh"
@@ -65,22 +65,19 @@ __global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const RopeArgs a
   const T* q = static_cast<const T*>(a.q) + tok * a.q_stride + lane * 8;
   const T* k = static_cast<const T*>(a.k) + tok * a.k_stride + lane * 8;
   Raw<T> raw[kAhead];
-  auto fetch = [&](int h) {
+  auto fetch = [&](int i, int r) {
+    if (r < h1) {
+      const uint4* src = reinterpret_cast<const uint4*>(r < a.q_heads ? q + (int64_t)r * D : k + (int64_t)(r - a.q_heads) * D);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int r = h + i * kRows + sub;
-      if (r < h1) {
-        const uint4* src = reinterpret_cast<const uint4*>(r < a.q_heads ? q + (int64_t)r * D : k + (int64_t)(r - a.q_heads) * D);
-#pragma unroll
-        for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[i].w[e] = src[e];
-      }
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[i].w[e] = __ldcs(src + e);
     }
   };
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i)
+  for (int i = 0; i < kAhead; ++i) {
 #pragma unroll
     for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[i].w[e] = make_uint4(0, 0, 0, 0);
-  fetch(h0);
+    fetch(i, h0 + i * kRows + sub);
+  }
   const int half = a.rotary / 2;
   const double pos = (double)a.pos[tok] * 0.31830988618379067154;                    // over pi
   for (int f = wl; f < half; f += 32) {
@@ -108,7 +105,6 @@ __global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const RopeArgs a
   T* qo = static_cast<T*>(a.q_out) + tok * a.q_out_stride + lane * 8;
   T* ko = static_cast<T*>(a.k_out) + tok * a.k_out_stride + lane * 8;
   for (int h = h0; h < h1; h += kAhead * kRows) {
-    if (h != h0) fetch(h);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (h + i * kRows >= h1) break;          // the same for the whole warp
@@ -116,6 +112,7 @@ __global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const RopeArgs a
       const bool is_q = r < a.q_heads;
       float x[8];
       unpack<T>(raw[i], x);
+      fetch(i, r + kAhead * kRows);            // in place of the rows just taken
       if (a.qw || a.kw) {
         float ss = 0.f;
 #pragma unroll

@@ -92,12 +92,6 @@ __device__ __forceinline__ void begin() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// Two e4m3 codes (low byte first) as fp32; exact.
-__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t codes) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), __NV_E4M3);
-  return __half22float2(__half2(h));
-}
-
 // One signed byte of a word as fp32, exact: a byte offset by 128 under the exponent of 2^23.
 __device__ __forceinline__ float i8_to_float(uint32_t offset_word, int i) {
   return __uint_as_float(__byte_perm(offset_word, 0x4B000000u, 0x7650 + i)) - 8388736.f;
@@ -107,7 +101,9 @@ __device__ __forceinline__ float i8_to_float(uint32_t offset_word, int i) {
 template <typename C>
 __device__ __forceinline__ void codes_to_float(uint32_t w, float (&f)[4]) {
   if constexpr (C::kTop == 448.f) {
-    const float2 a = e4m3x2_to_float2(w), b = e4m3x2_to_float2(w >> 16);
+    uint32_t lo, hi;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
     f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
   } else {
     const uint32_t o = w ^ 0x80808080u;
