@@ -2,17 +2,17 @@
 //
 //   y = x * rsqrt(mean(x^2) + eps) * w;   (a, b) -> (a cos - b sin, b cos + a sin),  angle = pos * inv_freq
 //
-// Every row (token, head) is read and written once, so the pass is bound by HBM. A row belongs to
-// d / 8 lanes of a warp, eight elements each; the mean square is a butterfly over those lanes, and with
-// paired halves an element's partner is eight elements of one other lane (rotary_dim / 2 is a multiple
-// of eight), fetched by a shuffle.
+// Every row (token, head) is read and written once, so the pass is bound by HBM. A lane has two runs of
+// eight elements of a row, d / 2 apart: paired halves of a fully rotated head then meet in one lane, as
+// neighbours always do, and four (d = 128) or eight rows share a warp's butterfly for the mean square. Where
+// only a part of a head is rotated by halves, a lane has one run and its partner's comes by shuffles.
 //
-// A warp takes a run of heads of ONE token, so that a lane's eight sines and cosines stay in registers
-// over all of them (read from shared memory per row they cost bank conflicts that took as long as the
-// traffic), and keeps the loads of four rounds of rows under way. Few tokens are cut into more runs, for
-// the sake of more warps. Angles are formed in fp64 (a position of a million times a
-// frequency near one leaves fp32 no digits after the point), reduced to half turns there, then sinpi and
-// cospi in fp32 (error below 1e-7); each lane forms some and the warp shares them.
+// A warp takes a run of heads of ONE token, so that sines, cosines and weights, multiplied into two
+// factors per element (of itself and of its partner), stay in registers over all of them, and keeps the
+// loads of four rounds of rows under way. Few tokens are cut into more runs, for the sake of more warps.
+// Angles are formed in fp64 (a position of a million times a frequency near one leaves fp32 no digits
+// after the point), reduced to half turns there, then sinpi and cospi in fp32 (error below 1e-7); each
+// lane forms some and the warp shares them.
 #include "paged_internal.cuh"
 
 namespace {
@@ -22,13 +22,15 @@ using namespace buzz_paged_dev;
 constexpr int kWarps = 4;
 constexpr int kAhead = 4;           // rounds of rows whose loads are under way together
 
+enum Pairs { kHalves, kHalvesInPart, kNeighbours };
+
 struct RopeArgs {
   const void *q, *k, *qw, *kw;
   void *q_out, *k_out;
   const int32_t* pos;
   const float* inv_freq;
   int64_t q_stride, k_stride, q_out_stride, k_out_stride;
-  int tokens, q_heads, kv_heads, rotary, runs, run_heads;
+  int tokens, q_heads, kv_heads, rotary, runs, run_rounds;
   float eps;
 };
 
@@ -50,33 +52,47 @@ __device__ __forceinline__ void unpack(const Raw<T>& r, float (&x)[8]) {
   }
 }
 
-template <typename T, int D, bool kInterleaved>
+template <typename T, int D, Pairs kPairs>
+struct RopePlan {
+  static constexpr int kRuns = kPairs == kHalvesInPart ? 1 : 2;    // runs of eight elements of a lane
+  static constexpr int kLanes = D / 8 / kRuns;                     // lanes of a row
+  static constexpr int kRows = 32 / kLanes;                        // rows of a warp's round
+};
+
+template <typename T, int D, Pairs kPairs>
 __global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const RopeArgs a) {
-  constexpr int kLanes = D / 8;               // lanes of a row
-  constexpr int kRows = 32 / kLanes;          // rows of a warp's round
+  using L = RopePlan<T, D, kPairs>;
+  constexpr int kRuns = L::kRuns, kLanes = L::kLanes, kRows = L::kRows;
   __shared__ float2 turn[kWarps][D / 2];      // (cos, sin) of the warp's token
   begin();
   const int warp = threadIdx.x / 32, wl = threadIdx.x & 31, lane = wl % kLanes, sub = wl / kLanes;
   const int64_t unit = (int64_t)blockIdx.x * kWarps + warp;
   const int64_t tok = unit / a.runs;
   if (tok >= a.tokens) return;
-  const int h0 = (int)(unit - tok * a.runs) * a.run_heads;
-  const int h1 = min(h0 + a.run_heads, a.q_heads + a.kv_heads);
+  // rounds of a token: those of q, then those of k
+  const int q_rounds = (a.q_heads + kRows - 1) / kRows, all = q_rounds + (a.kv_heads + kRows - 1) / kRows;
+  const int first = (int)(unit - tok * a.runs) * a.run_rounds, last = min(first + a.run_rounds, all);
   const T* q = static_cast<const T*>(a.q) + tok * a.q_stride + lane * 8;
   const T* k = static_cast<const T*>(a.k) + tok * a.k_stride + lane * 8;
-  Raw<T> raw[kAhead];
-  auto fetch = [&](int i, int r) {
-    if (r < h1) {
-      const uint4* src = reinterpret_cast<const uint4*>(r < a.q_heads ? q + (int64_t)r * D : k + (int64_t)(r - a.q_heads) * D);
+  Raw<T> raw[kAhead][kRuns];
+  auto fetch = [&](int i, int round) {
+    if (round >= last) return;
+    const bool is_q = round < q_rounds;
+    const int r = (is_q ? round : round - q_rounds) * kRows + sub;
+    if (r >= (is_q ? a.q_heads : a.kv_heads)) return;
+    const T* src = (is_q ? q : k) + (int64_t)r * D;
 #pragma unroll
-      for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[i].w[e] = __ldcs(src + e);
-    }
+    for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[i][c].w[e] = __ldcs(reinterpret_cast<const uint4*>(src + c * (D / 2)) + e);
   };
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
 #pragma unroll
-    for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[i].w[e] = make_uint4(0, 0, 0, 0);
-    fetch(i, h0 + i * kRows + sub);
+    for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[i][c].w[e] = make_uint4(0, 0, 0, 0);
+    fetch(i, first + i);
   }
   const int half = a.rotary / 2;
   const double pos = (double)a.pos[tok] * 0.31830988618379067154;                    // over pi
@@ -87,61 +103,98 @@ __global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const RopeArgs a
     turn[warp][f] = make_float2(c, s);
   }
   __syncwarp();
-  // a lane's part of the rotation: element i times co[i] plus its partner times si[i]
-  const int hl = half / 8;                     // lanes of one half
-  const bool turned = kInterleaved ? lane * 8 < a.rotary : lane < 2 * hl;
-  const int mate = !turned ? lane : lane < hl ? lane + hl : lane - hl;
-  float co[8], si[8];
+  const int hl = half / 8;                     // lanes of one half, where a part is rotated by halves
+  const int mate = lane < hl ? lane + hl : lane < 2 * hl ? lane - hl : lane;
+  bool turned[kRuns];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int f = kInterleaved ? lane * 4 + i / 2 : (lane < hl ? lane : mate) * 8 + i;
-    const float2 cs = turned ? turn[warp][f] : make_float2(1.f, 0.f);
-    co[i] = cs.x;
-    si[i] = (kInterleaved ? i % 2 == 0 : lane < hl) ? -cs.y : cs.y;
-  }
-  float wq[8], wk[8];
-  if (a.qw) load8(static_cast<const T*>(a.qw) + lane * 8, wq);
-  if (a.kw) load8(static_cast<const T*>(a.kw) + lane * 8, wk);
-  T* qo = static_cast<T*>(a.q_out) + tok * a.q_out_stride + lane * 8;
-  T* ko = static_cast<T*>(a.k_out) + tok * a.k_out_stride + lane * 8;
-  for (int h = h0; h < h1; h += kAhead * kRows) {
+  for (int c = 0; c < kRuns; ++c) turned[c] = kPairs == kHalves || (kPairs == kNeighbours ? c * (D / 2) + lane * 8 < a.rotary : lane < 2 * hl);
+  float own[kRuns][8], other[kRuns][8];        // factors of an element and of its partner
+  bool normed = false;
+  auto factors = [&](const void* weight) {
+    normed = weight != nullptr;
+#pragma unroll
+    for (int c = 0; c < kRuns; ++c) {
+      float w[8], wp[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = wp[i] = 1.f;
+      if (normed) {
+        load8(static_cast<const T*>(weight) + c * (D / 2) + lane * 8, w);
+        load8(static_cast<const T*>(weight) + (kPairs == kHalves ? (1 - c) * (D / 2) + lane * 8 : kPairs == kNeighbours ? c * (D / 2) + lane * 8 : mate * 8), wp);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int f = kPairs == kHalves ? lane * 8 + i : kPairs == kNeighbours ? (c * (D / 2) + lane * 8 + i) / 2 : (lane < hl ? lane : mate) * 8 + i;
+        const bool low = kPairs == kHalves ? c == 0 : kPairs == kNeighbours ? i % 2 == 0 : lane < hl;
+        const float2 cs = turned[c] ? turn[warp][f] : make_float2(1.f, 0.f);
+        own[c][i] = w[i] * cs.x;
+        other[c][i] = (low ? -cs.y : cs.y) * wp[kPairs == kNeighbours ? i ^ 1 : i];
+      }
+    }
+  };
+  if (first < q_rounds) factors(a.qw);
+  for (int r0 = first; r0 < last; r0 += kAhead) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (h + i * kRows >= h1) break;          // the same for the whole warp
-      const int r = h + i * kRows + sub;
-      const bool is_q = r < a.q_heads;
-      float x[8];
-      unpack<T>(raw[i], x);
-      fetch(i, r + kAhead * kRows);            // in place of the rows just taken
-      if (a.qw || a.kw) {
+      const int round = r0 + i;
+      if (round >= last) break;                // the same for the whole warp
+      const bool is_q = round < q_rounds;
+      if (round == q_rounds || (round == first && !is_q)) factors(a.kw);
+      float x[kRuns][8], scale = 1.f;
+#pragma unroll
+      for (int c = 0; c < kRuns; ++c) unpack<T>(raw[i][c], x[c]);
+      fetch(i, round + kAhead);                // in place of the rows just taken
+      if (normed) {
         float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+        for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ss += x[c][e] * x[c][e];
 #pragma unroll
         for (int off = kLanes / 2; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-        const float inv = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-        if (is_q ? a.qw != nullptr : a.kw != nullptr) {
+        scale = rsqrtf(ss * (1.0f / D) + a.eps);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= inv * (is_q ? wq[e] : wk[e]);
+        for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[c][e] *= scale;
+      }
+      float y[kRuns][8];
+#pragma unroll
+      for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float p;
+          if constexpr (kPairs == kHalves) p = x[1 - c][e];
+          else if constexpr (kPairs == kNeighbours) p = x[c][e ^ 1];
+          else p = __shfl_sync(0xffffffffu, x[c][e], mate, kLanes);
+          y[c][e] = turned[c] ? x[c][e] * own[c][e] + p * other[c][e] : x[c][e] * own[c][e];
         }
-      }
-      float y[8];
+      const int r = (is_q ? round : round - q_rounds) * kRows + sub;
+      if (r < (is_q ? a.q_heads : a.kv_heads)) {
+        T* dst = is_q ? static_cast<T*>(a.q_out) + tok * a.q_out_stride : static_cast<T*>(a.k_out) + tok * a.k_out_stride;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float other;
-        if constexpr (kInterleaved) other = x[e ^ 1];
-        else other = __shfl_sync(0xffffffffu, x[e], mate, kLanes);
-        y[e] = turned ? x[e] * co[e] + other * si[e] : x[e];
+        for (int c = 0; c < kRuns; ++c) store8(dst + (int64_t)r * D + c * (D / 2) + lane * 8, y[c]);
       }
-      if (r < h1) store8(is_q ? qo + (int64_t)r * D : ko + (int64_t)(r - a.q_heads) * D, y);
     }
   }
 }
 
+template <typename T, int D, Pairs kPairs>
+cudaError_t launch_pairs(RopeArgs a, cudaStream_t s) {
+  using L = RopePlan<T, D, kPairs>;
+  // A run is a whole token where there are warps enough without cutting one (16 for each of 148 SMs), and at
+  // least one round of rows.
+  const int all = (a.q_heads + L::kRows - 1) / L::kRows + (a.kv_heads + L::kRows - 1) / L::kRows;
+  const int want = (16 * 148 + a.tokens - 1) / a.tokens, runs = want < all ? want : all;
+  a.run_rounds = (all + runs - 1) / runs;
+  a.runs = (all + a.run_rounds - 1) / a.run_rounds;
+  const int64_t blocks = ((int64_t)a.tokens * a.runs + kWarps - 1) / kWarps;       // below 2^31: a token has one run if there are many
+  return buzz_launch_chained(norm_rope_kernel<T, D, kPairs>, dim3((unsigned)blocks), kWarps * 32u, 0, s, a);
+}
+
 template <typename T, int D>
-cudaError_t launch(const RopeArgs& a, bool interleaved, unsigned blocks, cudaStream_t s) {
-  if (interleaved) return buzz_launch_chained(norm_rope_kernel<T, D, true>, dim3(blocks), kWarps * 32u, 0, s, a);
-  return buzz_launch_chained(norm_rope_kernel<T, D, false>, dim3(blocks), kWarps * 32u, 0, s, a);
+cudaError_t launch(const RopeArgs& a, bool interleaved, cudaStream_t s) {
+  if (interleaved) return launch_pairs<T, D, kNeighbours>(a, s);
+  return a.rotary == D ? launch_pairs<T, D, kHalves>(a, s) : launch_pairs<T, D, kHalvesInPart>(a, s);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -165,22 +218,15 @@ extern "C" int buzz_norm_rope(const buzz_rope_shape* sh, const void* q, const vo
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_weight) || !aligned16(k_weight) ||
       (reinterpret_cast<uintptr_t>(positions_dev) | reinterpret_cast<uintptr_t>(inv_freq_dev)) & 3u)
     return BUZZ_ERR_INVALID;
-  // A run is a whole token where there are warps enough without cutting one (16 for each of 148 SMs), and at
-  // least one round of rows.
-  const int heads = sh->q_heads + sh->kv_heads, rows = 32 / (sh->head_dim / 8), rounds = (heads + rows - 1) / rows;
-  const int want = (16 * 148 + tokens - 1) / tokens;
-  const int per = (rounds + (want < rounds ? want : rounds) - 1) / (want < rounds ? want : rounds);
-  RopeArgs a{q, k, q_weight, k_weight, q_out, k_out, positions_dev, inv_freq_dev, sh->q_stride, sh->k_stride, sh->q_out_stride,
-             sh->k_out_stride, tokens, sh->q_heads, sh->kv_heads, sh->rotary_dim, (rounds + per - 1) / per, per * rows, sh->eps};
-  const int64_t blocks = ((int64_t)tokens * a.runs + kWarps - 1) / kWarps;
-  if (blocks > 0x7fffffff) return BUZZ_ERR_TOO_LARGE;
+  const RopeArgs a{q, k, q_weight, k_weight, q_out, k_out, positions_dev, inv_freq_dev, sh->q_stride, sh->k_stride, sh->q_out_stride,
+                   sh->k_out_stride, tokens, sh->q_heads, sh->kv_heads, sh->rotary_dim, 1, 1, sh->eps};
   (void)cudaGetLastError();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool il = sh->interleaved != 0;
   cudaError_t e;
   if (sh->dtype == BUZZ_BF16)
-    e = sh->head_dim == 128 ? launch<__nv_bfloat16, 128>(a, il, (unsigned)blocks, s) : launch<__nv_bfloat16, 64>(a, il, (unsigned)blocks, s);
+    e = sh->head_dim == 128 ? launch<__nv_bfloat16, 128>(a, il, s) : launch<__nv_bfloat16, 64>(a, il, s);
   else
-    e = sh->head_dim == 128 ? launch<float, 128>(a, il, (unsigned)blocks, s) : launch<float, 64>(a, il, (unsigned)blocks, s);
+    e = sh->head_dim == 128 ? launch<float, 128>(a, il, s) : launch<float, 64>(a, il, s);
   return e == cudaSuccess ? BUZZ_OK : BUZZ_ERR_CUDA;
 }

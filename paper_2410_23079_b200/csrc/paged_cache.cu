@@ -1,8 +1,8 @@
 // Rows into the pages and out of them.
 //
 // append: a warp owns one (sequence, touched page, KV head) and walks the page's new rows, K and V
-// together; a row belongs to d / 8 lanes, eight elements each, so that a row is one 16-byte (bf16) or
-// 32-byte (fp32) load per lane, and the next rows are under way while one is worked on. 8-bit caches take
+// together; a row belongs to d / 16 lanes, two runs of eight elements each (what a row costs once, the
+// butterfly and the scale, is then shared by more rows), and the next rows are under way while one is worked on. 8-bit caches take
 // the row's largest magnitude by a butterfly over its lanes, on the bit patterns (as unsigned numbers a NaN
 // is above every infinity, so it is not lost). A code is the rounding of an fp32 quotient, decided at the
 // border between two codes; the quotient is estimated by a product with the scale's reciprocal (off by
@@ -73,19 +73,22 @@ __device__ __forceinline__ void unpack(const Raw<T>& r, float (&x)[8]) {
 }
 // Bits of the largest magnitude of a row, as fp32; NaN counts as the largest.
 template <typename T, int kLanes>
-__device__ __forceinline__ uint32_t row_top(const Raw<T>& r) {
+__device__ __forceinline__ uint32_t row_top(const Raw<T> (&r)[2]) {
   uint32_t top = 0;
   if constexpr (sizeof(T) == 2) {                // two at a time
-    const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+    for (int c = 0; c < 2; ++c)
+      top = __vmaxu2(top, __vmaxu2(__vmaxu2(r[c].w[0].x & 0x7fff7fffu, r[c].w[0].y & 0x7fff7fffu),
+                                   __vmaxu2(r[c].w[0].z & 0x7fff7fffu, r[c].w[0].w & 0x7fff7fffu)));
 #pragma unroll
     for (int off = kLanes / 2; off > 0; off >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, off));
     return max(top << 16, top & 0xffff0000u);
   } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      top = max(top, max(max(r.w[i].x & 0x7fffffffu, r.w[i].y & 0x7fffffffu), max(r.w[i].z & 0x7fffffffu, r.w[i].w & 0x7fffffffu)));
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        top = max(top, max(max(r[c].w[i].x & 0x7fffffffu, r[c].w[i].y & 0x7fffffffu), max(r[c].w[i].z & 0x7fffffffu, r[c].w[i].w & 0x7fffffffu)));
 #pragma unroll
     for (int off = kLanes / 2; off > 0; off >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
     return top;
@@ -123,33 +126,39 @@ __device__ __forceinline__ uint2 encode(const float (&y)[8], bool& near) {
   return make_uint2(w[0], w[1]);
 }
 
-// Stores eight elements of one row; `kLanes` lanes hold the row.
+// Stores a lane's elements of one row; `kLanes` lanes hold the row, two runs of eight each.
 template <typename T, typename C, int kLanes>
-__device__ __forceinline__ void put_row(char* cache, float* scales, size_t row, int lane, const Raw<T>& raw, const float (&x)[8], bool on) {
+__device__ __forceinline__ void put_row(char* cache, float* scales, size_t row, int lane, const Raw<T> (&raw)[2], bool on) {
   if constexpr (C::kScaled) {
     float scale = __fdiv_rn(__uint_as_float(row_top<T, kLanes>(raw)), C::kTop);
     constexpr float kTiny = 7.888609052210118e-31f;          // 2^-100: a row of zeros has codes of zero
     if (scale < kTiny) scale = kTiny;                         // false for NaN, which stays
     if (!on) return;
     const float inv = __frcp_rn(scale);
-    float y[8];
-    bool near = false, never = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x[e] * inv;
-    uint2 w = encode<C>(y, near);
-    if (near) {
+    for (int c = 0; c < 2; ++c) {
+      float x[8], y[8];
+      bool near = false, never = false;
+      unpack(raw[c], x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = __fdiv_rn(x[e], scale);
-      w = encode<C>(y, never);
+      for (int e = 0; e < 8; ++e) y[e] = x[e] * inv;
+      uint2 w = encode<C>(y, near);
+      if (near) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __fdiv_rn(x[e], scale);
+        w = encode<C>(y, never);
+      }
+      if (!(scale <= 3.402823466e38f)) w = make_uint2(0, 0);   // infinity or NaN: times zero it reads back as NaN
+      reinterpret_cast<uint2*>(cache + row * (kLanes * 16))[c * kLanes + lane] = w;
     }
-    if (!(scale <= 3.402823466e38f)) w = make_uint2(0, 0);     // infinity or NaN: times zero it reads back as NaN
-    reinterpret_cast<uint2*>(cache + row * (kLanes * 8))[lane] = w;
     if (lane == 0) scales[row] = scale;
   } else {
     if (!on) return;
-    uint4* dst = reinterpret_cast<uint4*>(cache) + (row * kLanes + lane) * (sizeof(T) / 2);
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) dst[i] = raw.w[i];
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+        reinterpret_cast<uint4*>(cache)[((row * 2 + c) * kLanes + lane) * (sizeof(T) / 2) + i] = raw[c].w[i];
   }
 }
 
@@ -188,7 +197,7 @@ template <typename T, typename C, int D>
 __global__ void __launch_bounds__(kWarps * 32)
 append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ v, const int32_t* cu, int total_tokens, int max_new,
               const int32_t* lens, const int32_t* table, int table_stride, int touched) {
-  constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes;
   begin();
   const int item = blockIdx.x * kWarps + threadIdx.x / 32;
   const int b = blockIdx.y, j = item / w.kv_heads, h = item - j * w.kv_heads;
@@ -197,48 +206,59 @@ append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ 
   Span s;
   if (!find_span(w, cu, total_tokens, max_new, lens, table, table_stride, b, j, wl, s)) return;
   const size_t base = ((size_t)s.page * w.kv_heads + h) << w.page_log2;
-  float lo[8], hi[8];
+  float lo[2][8], hi[2][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { lo[c][i] = INFINITY; hi[c][i] = -INFINITY; }
   const size_t src = ((size_t)(s.src + sub) * w.kv_heads + h) * D + lane * 8, step = (size_t)kRows * w.kv_heads * D;
-  Raw<T> kn = {}, vn = {};                             // the next rows, under way while these are worked on
-  if (s.slot0 + sub < s.slot1) { fetch8(k + src, kn); fetch8(v + src, vn); }
+  Raw<T> kn[2] = {}, vn[2] = {};                       // the next rows, under way while these are worked on
+  auto fetch = [&](size_t at) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) { fetch8(k + at + c * (D / 2), kn[c]); fetch8(v + at + c * (D / 2), vn[c]); }
+  };
+  if (s.slot0 + sub < s.slot1) fetch(src);
   size_t ahead = src + step;
   for (int r0 = s.slot0; r0 < s.slot1; r0 += kRows, ahead += step) {
     const int r = r0 + sub;
     const bool on = r < s.slot1;
-    const Raw<T> kr = kn, vr = vn;
-    if (r + kRows < s.slot1) { fetch8(k + ahead, kn); fetch8(v + ahead, vn); }
-    float x[8], y[8];
-    unpack(kr, x);
-    unpack(vr, y);
+    const Raw<T> kr[2] = {kn[0], kn[1]}, vr[2] = {vn[0], vn[1]};
+    if (r + kRows < s.slot1) fetch(ahead);
     if (w.bounds != nullptr && on) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { lo[i] = fminf(lo[i], x[i]); hi[i] = fmaxf(hi[i], x[i]); }
+      for (int c = 0; c < 2; ++c) {
+        float x[8];
+        unpack(kr[c], x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { lo[c][i] = fminf(lo[c][i], x[i]); hi[c][i] = fmaxf(hi[c][i], x[i]); }
+      }
     }
-    put_row<T, C, kLanes>(w.k, w.k_scale, base + r, lane, kr, x, on);
-    put_row<T, C, kLanes>(w.v, w.v_scale, base + r, lane, vr, y, on);
+    put_row<T, C, kLanes>(w.k, w.k_scale, base + r, lane, kr, on);
+    put_row<T, C, kLanes>(w.v, w.v_scale, base + r, lane, vr, on);
   }
   if (w.bounds == nullptr) return;
-  T* bnd = reinterpret_cast<T*>(w.bounds) + ((size_t)s.page * w.kv_heads + h) * 2 * D + lane * 8;
-  if (s.slot0 > 0) {                                   // older rows: the stored bounds hold them
-    float a[8], c[8];
-    load8(bnd, a);
-    load8(bnd + D, c);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { lo[i] = fminf(lo[i], a[i]); hi[i] = fmaxf(hi[i], c[i]); }
-  }
+  for (int c = 0; c < 2; ++c) {
+    T* bnd = reinterpret_cast<T*>(w.bounds) + ((size_t)s.page * w.kv_heads + h) * 2 * D + c * (D / 2) + lane * 8;
+    if (s.slot0 > 0) {                                 // older rows: the stored bounds hold them
+      float p[8], q[8];
+      load8(bnd, p);
+      load8(bnd + D, q);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-#pragma unroll
-    for (int off = kLanes; off < 32; off <<= 1) {
-      lo[i] = fminf(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], off));
-      hi[i] = fmaxf(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], off));
+      for (int i = 0; i < 8; ++i) { lo[c][i] = fminf(lo[c][i], p[i]); hi[c][i] = fmaxf(hi[c][i], q[i]); }
     }
-  }
-  if (sub == 0) {
-    store8(bnd, lo);
-    store8(bnd + D, hi);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int off = kLanes; off < 32; off <<= 1) {
+        lo[c][i] = fminf(lo[c][i], __shfl_xor_sync(0xffffffffu, lo[c][i], off));
+        hi[c][i] = fmaxf(hi[c][i], __shfl_xor_sync(0xffffffffu, hi[c][i], off));
+      }
+    }
+    if (sub == 0) {
+      store8(bnd, lo[c]);
+      store8(bnd + D, hi[c]);
+    }
   }
 }
 
