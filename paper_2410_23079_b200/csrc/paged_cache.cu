@@ -7,8 +7,8 @@
 // is above every infinity, so it is not lost). A code is the rounding of an fp32 quotient, decided at the
 // border between two codes; the quotient is estimated by a product with the scale's reciprocal (off by
 // 2^-22 of itself at most) and divided out only where a border lies that near, so that the codes are those
-// of the division (which for every element cost more than the traffic: 220 us instead of 130 for 16 prompts
-// of 4096..8192 tokens). Because the whole page belongs to the warp, its bounds need no atomics: the
+// of the division (which for every element cost more than the traffic: 220 us instead of 140 for 16 prompts
+// of 4096..8192 tokens; dividing out single elements of a run instead of its eight is no faster). Because the whole page belongs to the warp, its bounds need no atomics: the
 // smallest and largest value per dimension are kept in registers over the rows and joined with the stored
 // ones only if the page has older rows.
 // read: the same walk, the other way, four rounds of rows at a time. Both are bound by the bytes they move.
@@ -18,7 +18,7 @@ namespace {
 
 using namespace buzz_paged_dev;
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 
 // What one warp works on; false: nothing.
 struct Span {
@@ -194,7 +194,7 @@ __device__ __forceinline__ void write_row(T* dst, const Kept<C>& r) {
 }
 
 template <typename T, typename C, int D>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 2 ? 6 : 4)
 append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ v, const int32_t* cu, int total_tokens, int max_new,
               const int32_t* lens, const int32_t* table, int table_stride, int touched) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes;
