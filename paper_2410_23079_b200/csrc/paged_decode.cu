@@ -41,6 +41,7 @@ using namespace buzz_paged_dev;
 
 constexpr int kHeads = 8;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr long long kWholeBytes = 512 << 10;
 constexpr float kSlack = 6.f;        // log2 of the largest probability before the maximum in use is raised
 constexpr float kUnit = 256.f;       // 8-bit caches: weight of a probability of 1 at the largest value scale; times 2^kSlack and 2, below 2^16
 
@@ -50,6 +51,7 @@ struct DecodeArgs {
   float* lse;
   const int32_t *lens, *table, *selected;
   int table_stride, selected_stride, batch, max_len, group, logn;
+  int whole;       // a block per (sequence, KV head): nothing is split, nothing joined
   float scale_log2;
   int4* desc;      // [blocks]: (instance whose join this block begins, or -1; last block of it)
   float* part;     // [blocks][2][part_floats]: outputs [group][D], maxima [8], sums [8]
@@ -247,63 +249,81 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   __shared__ int found[2];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
   for (int i = tid; i < L::kRing; i += kThreads) sm100::mbar_init(full + i, 1);
+  if (tid == 0) {
+    sm100::prefetch_tensormap(&k_map);
+    sm100::prefetch_tensormap(&v_map);
+  }
   sm100::fence_barrier_init();
   begin();
 
   // ---- the line of work, and this block's stretch of it ----------------------------------------
-  long long mine = 0;
-  const int per = (a.batch + kThreads - 1) / kThreads;
-  const int b_lo = min(tid * per, a.batch), b_hi = min(b_lo + per, a.batch);
-  for (int b = b_lo; b < b_hi; ++b) {
-    Place p;
-    set_sequence<L>(a, w, p, a.lens[b]);
-    mine += p.units;
-    if (p.bad && blockIdx.x == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, b, a.lens[b]);
-  }
-  long long incl = mine;
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const long long o = __shfl_up_sync(0xffffffffu, incl, off);
-    if (lane >= off) incl += o;
-  }
-  if (lane == 31) warp_sum[warp] = incl;
-  __syncthreads();
-  long long before = 0, total = 0;
-#pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) {
-    if (i < warp) before += warp_sum[i];
-    total += warp_sum[i];
-  }
-  const long long U = total * w.kv_heads;
-  const int n = (int)min((long long)gridDim.x, U);
-  if ((int)blockIdx.x >= n) {
-    if (tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    return;
-  }
-  const long long u_begin = blockIdx.x * U / n, u_end = (blockIdx.x + 1) * U / n;
-  {
-    long long ex = (before + incl - mine) * w.kv_heads;
-    if (u_begin >= ex && u_begin < ex + mine * w.kv_heads) {
-      Place p;
-      int b = b_lo;
-      for (;; ++b) {
-        set_sequence<L>(a, w, p, a.lens[b]);
-        const long long here = (long long)p.units * w.kv_heads;
-        if (u_begin < ex + here) break;
-        ex += here;
-      }
-      found[0] = b;
-      found[1] = (int)(u_begin - ex);
-    }
-  }
-  __syncthreads();
   Place cur;
-  cur.b = found[0];
-  set_sequence<L>(a, w, cur, a.lens[cur.b]);
-  cur.next = cur.b + 1 < a.batch ? a.lens[cur.b + 1] : 0;
-  cur.h = found[1] / cur.units;
-  cur.unit = found[1] - cur.h * cur.units;
-  const int n_units = (int)(u_end - u_begin);
+  int n = 0, n_units;
+  long long U = 0, u_begin = 0;
+  if (a.whole) {
+    cur.b = blockIdx.x / w.kv_heads;
+    cur.h = blockIdx.x - cur.b * w.kv_heads;
+    cur.unit = cur.next = 0;
+    const int len = a.lens[cur.b];
+    set_sequence<L>(a, w, cur, len);
+    if (cur.bad && cur.h == 0 && tid == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, cur.b, len);
+    n_units = cur.units;
+    __syncthreads();
+  } else {
+    long long mine = 0;
+    const int per = (a.batch + kThreads - 1) / kThreads;
+    const int b_lo = min(tid * per, a.batch), b_hi = min(b_lo + per, a.batch);
+    for (int b = b_lo; b < b_hi; ++b) {
+      Place p;
+      set_sequence<L>(a, w, p, a.lens[b]);
+      mine += p.units;
+      if (p.bad && blockIdx.x == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, b, a.lens[b]);
+    }
+    long long incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += o;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    long long before = 0, total = 0;
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) {
+      if (i < warp) before += warp_sum[i];
+      total += warp_sum[i];
+    }
+    U = total * w.kv_heads;
+    n = (int)min((long long)gridDim.x, U);
+    if ((int)blockIdx.x >= n) {
+      if (tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+      return;
+    }
+    u_begin = blockIdx.x * U / n;
+    const long long u_end = (blockIdx.x + 1) * U / n;
+    {
+      long long ex = (before + incl - mine) * w.kv_heads;
+      if (u_begin >= ex && u_begin < ex + mine * w.kv_heads) {
+        Place p;
+        int b = b_lo;
+        for (;; ++b) {
+          set_sequence<L>(a, w, p, a.lens[b]);
+          const long long here = (long long)p.units * w.kv_heads;
+          if (u_begin < ex + here) break;
+          ex += here;
+        }
+        found[0] = b;
+        found[1] = (int)(u_begin - ex);
+      }
+    }
+    __syncthreads();
+    cur.b = found[0];
+    set_sequence<L>(a, w, cur, a.lens[cur.b]);
+    cur.next = cur.b + 1 < a.batch ? a.lens[cur.b + 1] : 0;
+    cur.h = found[1] / cur.units;
+    cur.unit = found[1] - cur.h * cur.units;
+    n_units = (int)(u_end - u_begin);
+  }
 
   // ---- the ring: lane i looks up this warp's tile of every 32nd unit, from i on -------------------
   const int P = 1 << w.page_log2, box_rows = min(kTok, P);
@@ -719,7 +739,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
           if (x % (D / 4) == 0) { part[a.group * D + hd] = wt[hd]; part[a.group * D + kHeads + hd] = sum; }
         }
       }
-      if (u + 1 == n_units && tid == 0) {
+      if (u + 1 == n_units && tid == 0 && !a.whole) {
         // the join of an instance is described where the instance begins
         int4 d = make_int4(-1, 0, 0, 0);
         if (!complete && first_part) {
@@ -807,7 +827,11 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
   }
   const long long units = (tokens + L::kTok * L::kWarps - 1) / (L::kTok * L::kWarps);          // of a (sequence, KV head), at most
   const long long all = (long long)a.batch * c->sh.kv_heads * (units > 0 ? units : 1);
-  const int n = (int)(all < c->sm_count ? all : c->sm_count);
+  // Where a block could do each (sequence, KV head) alone, the join (a launch, 4 us on the host and 3 on the GPU) is
+  // not worth it: up to half a megabyte, which one SM reads in 4 us, and no more of them than SMs.
+  const long long heads = (long long)a.batch * c->sh.kv_heads;
+  a.whole = units * L::kWarps * 2 * L::kTileBytes <= kWholeBytes && heads <= c->sm_count;
+  const int n = (int)(a.whole ? heads : all < c->sm_count ? all : c->sm_count);
   const size_t smem = L::smem(c->group);
   static BuzzSmemOptIn opt_in;
   if (cudaError_t e = opt_in.ensure(paged_decode_kernel<T, C, D>, smem); e != cudaSuccess) return e;
@@ -815,7 +839,7 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
       e != cudaSuccess)
     return e;
   c->launches += 1;
-  if (units <= 1) return cudaSuccess;              // nothing is ever split
+  if (units <= 1 || a.whole) return cudaSuccess;   // nothing is split
   cudaError_t e = buzz_launch_chained(paged_join_kernel<T, D>, dim3(n), (unsigned)kJoinThreads, sizeof(float) * c->group * n, stream, a);
   if (e == cudaSuccess) c->launches += 1;
   return e;

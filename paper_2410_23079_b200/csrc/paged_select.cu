@@ -7,10 +7,12 @@
 // the group. What is read is 2 d elements per page, which HBM bounds. Sums are fp64: the pages around
 // the border are chosen or left out as a whole, and in fp32 the order of a sum would decide that.
 //
-// score_kernel: a block takes a run of pages of one (sequence, KV head); a page belongs to some lanes of
-//   a warp, 16 bytes each, and eight pages' loads are under way at once. Scores are left as unsigned keys that sort like the scores.
-// pick_kernel: one block per (sequence, KV head) finds the top-th largest key and writes the pages
-//   ascending (equal keys: the lowest pages).
+// A page belongs to some lanes of a warp, 16 bytes each, and eight pages' loads are under way at once. Scores
+// become unsigned keys that sort like the scores; the top-th largest key is found by histograms, and the
+// pages are written ascending (equal keys: the lowest pages).
+//   select_kernel: one block per (sequence, KV head) scores its pages into shared memory and picks: one launch,
+//     for few pages.
+//   score_kernel, pick_kernel: the pages of a (sequence, KV head) spread over blocks, keys in the workspace.
 #include "paged_internal.cuh"
 
 namespace {
@@ -32,7 +34,6 @@ __device__ __forceinline__ unsigned long long ordered_key(double x) {
   return (u >> 63) ? ~u : u | 0x8000000000000000ull;
 }
 
-constexpr int kScoreWarps = 4;
 constexpr int kBatch = 8;            // pages of a lane group whose bounds are under way together
 
 template <typename T, int D>
@@ -41,9 +42,7 @@ struct ScorePlan {
   static constexpr int kChunks = 2 * D / kE;                       // 16-byte chunks of a page's bounds
   static constexpr int kLanes = kChunks < 32 ? kChunks : 32;       // lanes of a page
   static constexpr int kCL = kChunks / kLanes;                     // chunks per lane
-  static constexpr int kPages = 32 / kLanes;                       // lane groups of a warp
-  static constexpr int kBatches = kLanes / kBatch;                 // a lane looks up one page of its group
-  static constexpr int kPerBlock = kScoreWarps * 32;
+  static constexpr int kBatches = kLanes / kBatch;                 // a lane looks up one page of its group: 32 pages a warp
 };
 
 template <typename T>
@@ -56,40 +55,37 @@ __device__ __forceinline__ void widen(const uint4& u, float (&x)[16 / sizeof(T)]
   }
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView w, const SelectArgs a) {
-  using L = ScorePlan<T, D>;
-  constexpr int kE = L::kE, kLanes = L::kLanes, kCL = L::kCL;
-  begin();
-  const int b = blockIdx.z, h = blockIdx.y;
-  const int len = a.lens[b];
-  if (len < 0 || len > a.max_len) return;                   // the pick records it
-  const int count = (len + (1 << w.page_log2) - 1) >> w.page_log2;
-  if (count <= a.sink + a.recent + a.top) return;
-  const int tid = threadIdx.x, warp = tid / 32, wl = tid & 31, lane = wl % kLanes, sub = wl / kLanes;
-  const int end = count - a.recent, block0 = a.sink + blockIdx.x * L::kPerBlock;
-  if (block0 >= end) return;
-  // lane i of a group looks up page i of the group's run
-  const int p0 = block0 + warp * 32 + sub * kLanes;
-  int mine = -1;
-  if (p0 + lane < end) {
-    mine = a.table[(int64_t)b * a.table_stride + p0 + lane];
-    if (mine < 0 || mine >= w.pages) {
-      buzz_set_status(w.status, BUZZ_ERR_INVALID, b, mine);
-      mine = -1;
-    }
-  }
-  // the group's queries by sign, once per block
-  __shared__ double qsum[2 * D];
-  for (int i = tid; i < 2 * D; i += kScoreWarps * 32) {
-    const T* q = static_cast<const T*>(a.q) + ((size_t)b * w.kv_heads + h) * a.group * D + i % D;
+// The group's queries by sign, summed, for the smallest values and then the largest: qsum[2 * D], by all threads.
+template <typename T, int D, int kThreads>
+__device__ __forceinline__ void sum_queries(const SelectArgs& a, int kv_heads, int b, int h, double* qsum) {
+  for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
+    const T* q = static_cast<const T*>(a.q) + ((size_t)b * kv_heads + h) * a.group * D + i % D;
     double sum = 0.0;
     for (int g = 0; g < a.group; ++g) {
       const float x = (float)q[g * D];
-      sum += (double)((x < 0.f) == (i < D) || x != x ? x : 0.f);    // the first half of the bounds is the smallest values
+      sum += (double)((x < 0.f) == (i < D) || x != x ? x : 0.f);
     }
     qsum[i] = sum;
   }
+}
+
+// The physical page of a lane's logical page, -1 (recorded) if it is none.
+__device__ __forceinline__ int look_up(const PagedView& w, const SelectArgs& a, int b, int lp, bool on) {
+  if (!on) return -1;
+  const int page = a.table[(int64_t)b * a.table_stride + lp];
+  if (page >= 0 && page < w.pages) return page;
+  buzz_set_status(w.status, BUZZ_ERR_INVALID, b, page);
+  return -1;
+}
+
+// Keys of the 32 pages from lp0 on (those below `end`), by one warp; `mine` is the physical page of lane i's page.
+// `put(i, key)` takes the key of logical page i.
+template <typename T, int D, typename Put>
+__device__ __forceinline__ void score_pages(const PagedView& w, int h, int lp0, int end, int mine, const double* qsum, Put&& put) {
+  using L = ScorePlan<T, D>;
+  constexpr int kE = L::kE, kLanes = L::kLanes, kCL = L::kCL;
+  const int wl = threadIdx.x & 31, lane = wl % kLanes, sub = wl / kLanes;
+  const int p0 = lp0 + sub * kLanes;                        // the lane group's pages
   uint4 raw[kBatch][kCL];
   auto fetch = [&](int batch) {
 #pragma unroll
@@ -101,25 +97,23 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView
     }
   };
   fetch(0);
-  __syncthreads();
-  double qs[kCL][kE];
-#pragma unroll
-  for (int c = 0; c < kCL; ++c)
-#pragma unroll
-    for (int e = 0; e < kE; ++e) qs[c][e] = qsum[(lane + c * kLanes) * kE + e];
 #pragma unroll 1
   for (int batch = 0; batch < L::kBatches; ++batch) {
-    if (block0 + warp * 32 + batch * kBatch >= end) break;    // nothing left for any group of the warp
+    if (lp0 + batch * kBatch >= end) break;                 // nothing left for any group of the warp
     double s[kBatch];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      s[i] = 0.0;
+    for (int i = 0; i < kBatch; ++i) s[i] = 0.0;
 #pragma unroll
-      for (int c = 0; c < kCL; ++c) {
+    for (int c = 0; c < kCL; ++c) {
+      double qs[kE];
+#pragma unroll
+      for (int e = 0; e < kE; ++e) qs[e] = qsum[(lane + c * kLanes) * kE + e];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
         float x[kE];
         widen<T>(raw[i][c], x);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) s[i] += qs[c][e] * (double)x[e];
+        for (int e = 0; e < kE; ++e) s[i] += qs[e] * (double)x[e];
       }
     }
     if (batch + 1 < L::kBatches) fetch(batch + 1);
@@ -137,62 +131,87 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView
     }
 #pragma unroll
     for (; off > 0; off >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], off);
-    constexpr int kRest = kLanes / kBatch;                    // lanes that now hold one page's sum
+    constexpr int kRest = kLanes / kBatch;                  // lanes that now hold one page's sum
     const int i = batch * kBatch + lane / kRest;
     const int page = __shfl_sync(0xffffffffu, mine, i, kLanes);
-    if (lane % kRest == 0 && p0 + i < end)
-      a.keys[((size_t)b * w.kv_heads + h) * a.max_pages + p0 + i] = page >= 0 ? ordered_key(s[0]) : 0;      // a bad page is below all others
+    if (lane % kRest == 0 && p0 + i < end) put(p0 + i, page >= 0 ? ordered_key(s[0]) : 0ull);      // a bad page is below all others
   }
 }
 
-// The pick: a block per (sequence, KV head). A histogram of kBins equal bins over the keys' range finds the
-// bin that holds the border; its keys (a handful where the scores spread) are ranked against one another,
-// and the one of the wanted rank is the last that is kept. A crowded bin is cut into kBins once more, down
-// to single values; pages of one value are ranked by their number.
-constexpr int kPickThreads = 1024;
-constexpr int kPickWarps = kPickThreads / 32;
-constexpr int kBins = 2 * kPickThreads;
-constexpr int kHeld = 8;             // keys a thread keeps in registers; more are read again each time
+constexpr int kScoreWarps = 4;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView w, const SelectArgs a) {
+  begin();
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int len = a.lens[b];
+  if (len < 0 || len > a.max_len) return;                   // the pick records it
+  const int count = (len + (1 << w.page_log2) - 1) >> w.page_log2;
+  if (count <= a.sink + a.recent + a.top) return;
+  const int end = count - a.recent, block0 = a.sink + blockIdx.x * (kScoreWarps * 32);
+  if (block0 >= end) return;
+  __shared__ double qsum[2 * D];
+  const int lp0 = block0 + (threadIdx.x & ~31), lp = lp0 + (threadIdx.x & 31);
+  const int mine = look_up(w, a, b, lp, lp < end);
+  sum_queries<T, D, kScoreWarps * 32>(a, w.kv_heads, b, h, qsum);
+  __syncthreads();
+  if (lp0 >= end) return;
+  unsigned long long* keys = a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages;
+  score_pages<T, D>(w, h, lp0, end, mine, qsum, [&](int i, unsigned long long key) { keys[i] = key; });
+}
+
+// The pick, by one block. A histogram of kBins equal bins over the keys' range finds the bin that holds the
+// border; its keys (a handful where the scores spread) are ranked against one another, and the one of the
+// wanted rank is the last that is kept. A crowded bin is cut into kBins once more, down to single values;
+// pages of one value are ranked by their number.
+constexpr int kBins = 2048;
 constexpr int kRanked = 256;         // keys that are ranked directly
 
-__global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, const SelectArgs a) {
-  typedef unsigned long long u64;
-  __shared__ int hist[kBins];
-  __shared__ u64 ends[2][kPickWarps];
-  __shared__ u64 cand[kRanked];
-  __shared__ int cand_at[kRanked];
-  __shared__ int cnt[kPickWarps];
-  __shared__ int border, border_rest, border_count, cand_n, last_at;
-  __shared__ u64 last_key;
-  begin();
-  const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
-  const int len = a.lens[b];
+template <int kThreads>
+struct PickSpace {
+  int hist[kBins];
+  unsigned long long ends[2][kThreads / 32], cand[kRanked], last_key;
+  int cand_at[kRanked], cnt[32], border, border_rest, border_count, cand_n, last_at;
+};
+
+// What is settled without scores: the pages of a sequence that keeps all, or the ends of one that does not.
+// Returns the number of pages in between that compete, 0 if there is nothing left to do.
+template <int kThreads>
+__device__ __forceinline__ int pick_ends(const PagedView& w, const SelectArgs& a, int b, int h, int32_t*& out) {
+  const int tid = threadIdx.x, len = a.lens[b];
   if (len < 0 || len > a.max_len) {
     if (tid == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, b, len);
-    return;
+    return 0;
   }
   const int count = (len + (1 << w.page_log2) - 1) >> w.page_log2;
   const int most = a.sink + a.recent + a.top;
-  int32_t* out = a.selected + ((size_t)b * w.kv_heads + h) * most;
+  out = a.selected + ((size_t)b * w.kv_heads + h) * most;
   if (count <= most) {
-    for (int i = tid; i < most; i += kPickThreads) out[i] = i < count ? i : -1;
-    return;
+    for (int i = tid; i < most; i += kThreads) out[i] = i < count ? i : -1;
+    return 0;
   }
-  for (int i = tid; i < a.sink; i += kPickThreads) out[i] = i;
-  for (int i = tid; i < a.recent; i += kPickThreads) out[a.sink + a.top + i] = count - a.recent + i;
-  if (a.top == 0) return;
-  // key i of the thread is that of page i * kPickThreads + tid of the middle
-  const u64* keys = a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages + a.sink;
-  const int n = count - a.recent - a.sink;
-  u64 held[kHeld];
+  for (int i = tid; i < a.sink; i += kThreads) out[i] = i;
+  for (int i = tid; i < a.recent; i += kThreads) out[a.sink + a.top + i] = count - a.recent + i;
+  out += a.sink;
+  return a.top == 0 ? 0 : count - a.recent - a.sink;
+}
+
+// Writes the numbers (plus `first`) of the `top` largest of n keys to out, ascending; top < n.
+template <int kThreads, int kHeld>
+__device__ __forceinline__ void pick_largest(const unsigned long long* keys, int n, int top, int first, int32_t* out, PickSpace<kThreads>& sp) {
+  typedef unsigned long long u64;
+  constexpr int kWarps = kThreads / 32, kOwn = kBins / kThreads;       // bins of a thread
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
+  // key i of the thread is that of page i * kThreads + tid; the first kHeld are kept in registers
+  u64 held[kHeld > 0 ? kHeld : 1];
   u64 small = ~0ull, large = 0;
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) held[i] = i * kPickThreads + tid < n ? keys[i * kPickThreads + tid] : 0;
+  for (int i = 0; i < kHeld; ++i) held[i] = i * kThreads + tid < n ? keys[i * kThreads + tid] : 0;
   auto each = [&](auto&& f) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
-      if (i * kPickThreads + tid < n) f(held[i], i * kPickThreads + tid);
-    for (int i = kHeld * kPickThreads + tid; i < n; i += kPickThreads) f(keys[i], i);
+      if (i * kThreads + tid < n) f(held[i], i * kThreads + tid);
+    for (int i = kHeld * kThreads + tid; i < n; i += kThreads) f(keys[i], i);
   };
   each([&](u64 k, int) { small = min(small, k); large = max(large, k); });
 #pragma unroll
@@ -200,123 +219,182 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, c
     small = min(small, __shfl_xor_sync(0xffffffffu, small, off));
     large = max(large, __shfl_xor_sync(0xffffffffu, large, off));
   }
-  if (lane == 0) { ends[0][warp] = small; ends[1][warp] = large; }
-  hist[tid] = hist[tid + kPickThreads] = 0;
-  if (tid == 0) cand_n = 0;
-  __syncthreads();
-  small = ends[0][lane];
-  large = ends[1][lane];
+  if (lane == 0) { sp.ends[0][warp] = small; sp.ends[1][warp] = large; }
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
+  for (int i = 0; i < kOwn; ++i) sp.hist[i * kThreads + tid] = 0;
+  if (tid == 0) sp.cand_n = 0;
+  __syncthreads();
+  small = sp.ends[0][lane % kWarps];
+  large = sp.ends[1][lane % kWarps];
+#pragma unroll
+  for (int off = kWarps / 2; off > 0; off >>= 1) {
     small = min(small, __shfl_xor_sync(0xffffffffu, small, off));
     large = max(large, __shfl_xor_sync(0xffffffffu, large, off));
   }
   u64 base = small, span = large - small;        // keys base .. base + span hold the border
-  int rest = a.top, shift;                       // how many of them are kept
+  int rest = top, shift;                         // how many of them are kept
   for (;;) {
     shift = max(0, 64 - __clzll((long long)span) - 11);
-    each([&](u64 k, int) { if (k - base <= span) atomicAdd(&hist[(int)((k - base) >> shift)], 1); });
+    each([&](u64 k, int) { if (k - base <= span) atomicAdd(&sp.hist[(int)((k - base) >> shift)], 1); });
     __syncthreads();
-    // bins from the top: thread t has bins kBins - 1 - 2t and the one below it
-    const int c0 = hist[kBins - 1 - 2 * tid], c1 = hist[kBins - 2 - 2 * tid];
-    int incl = c0 + c1;
+    // bins from the top: thread t has kOwn of them, from kBins - 1 - kOwn t downwards
+    int c[kOwn], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) { c[i] = sp.hist[kBins - 1 - kOwn * tid - i]; sum += c[i]; }
+    int incl = sum;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
       const int o = __shfl_up_sync(0xffffffffu, incl, off);
       if (lane >= off) incl += o;
     }
-    if (lane == 31) cnt[warp] = incl;
+    if (lane == 31) sp.cnt[warp] = incl;
     __syncthreads();
-    hist[kBins - 1 - 2 * tid] = hist[kBins - 2 - 2 * tid] = 0;
-    int over = incl - c0 - c1 + (int)__reduce_add_sync(0xffffffffu, lane < warp ? cnt[lane] : 0);
-    if (over < rest && rest <= over + c0 + c1) {
-      const bool second = rest > over + c0;
-      border = kBins - 1 - 2 * tid - (second ? 1 : 0);
-      border_rest = rest - over - (second ? c0 : 0);
-      border_count = second ? c1 : c0;
+    int over = incl - sum + (int)__reduce_add_sync(0xffffffffu, lane < warp ? sp.cnt[lane] : 0);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      sp.hist[kBins - 1 - kOwn * tid - i] = 0;
+      if (over < rest && rest <= over + c[i]) {
+        sp.border = kBins - 1 - kOwn * tid - i;
+        sp.border_rest = rest - over;
+        sp.border_count = c[i];
+      }
+      over += c[i];
     }
     __syncthreads();
-    base += (u64)border << shift;
+    base += (u64)sp.border << shift;
     span = (1ull << shift) - 1;
-    rest = border_rest;
-    if (border_count <= kRanked || shift == 0) break;
+    rest = sp.border_rest;
+    if (sp.border_count <= kRanked || shift == 0) break;
   }
   // the last key that is kept: the one of rank `rest` in the border's bin
-  if (border_count <= kRanked) {
+  const int crowd = sp.border_count;
+  if (crowd <= kRanked) {
     each([&](u64 k, int i) {
       if (k - base <= span) {
-        const int at = atomicAdd(&cand_n, 1);
-        cand[at] = k;
-        cand_at[at] = i;
+        const int at = atomicAdd(&sp.cand_n, 1);
+        sp.cand[at] = k;
+        sp.cand_at[at] = i;
       }
     });
     __syncthreads();
-    const int c = border_count;
-    if (tid < c) {
+    for (int c = tid; c < crowd; c += kThreads) {
       int rank = 0;
-      for (int x = 0; x < c; ++x) rank += cand[x] > cand[tid] || (cand[x] == cand[tid] && cand_at[x] < cand_at[tid]);
-      if (rank == rest - 1) { last_key = cand[tid]; last_at = cand_at[tid]; }
+      for (int x = 0; x < crowd; ++x) rank += sp.cand[x] > sp.cand[c] || (sp.cand[x] == sp.cand[c] && sp.cand_at[x] < sp.cand_at[c]);
+      if (rank == rest - 1) { sp.last_key = sp.cand[c]; sp.last_at = sp.cand_at[c]; }
     }
   } else {                                       // one value: the page of that rank among its pages
     int seen = 0;
-    for (int i0 = 0; i0 < n; i0 += kPickThreads) {
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
       const bool eq = i0 + tid < n && keys[i0 + tid] == base;
       const unsigned bal = __ballot_sync(0xffffffffu, eq);
-      if (lane == 0) cnt[warp] = __popc(bal);
+      if (lane == 0) sp.cnt[warp] = __popc(bal);
       __syncthreads();
-      const int before = seen + (int)__reduce_add_sync(0xffffffffu, lane < warp ? cnt[lane] : 0) + __popc(bal & ((1u << lane) - 1));
-      seen += (int)__reduce_add_sync(0xffffffffu, cnt[lane]);
-      if (eq && before == rest - 1) { last_key = base; last_at = i0 + tid; }
+      const int c = lane < kWarps ? sp.cnt[lane] : 0;
+      const int before = seen + (int)__reduce_add_sync(0xffffffffu, lane < warp ? c : 0) + __popc(bal & ((1u << lane) - 1));
+      seen += (int)__reduce_add_sync(0xffffffffu, c);
+      if (eq && before == rest - 1) { sp.last_key = base; sp.last_at = i0 + tid; }
       __syncthreads();
     }
   }
   __syncthreads();
-  // the kept pages in order: ranks of kHeld rows of pages at a time (hist is free: a count per row and warp)
-  const u64 lk = last_key;
-  const int la = last_at;
+  // the kept pages in order: ranks of kTurn rows of pages at a time (hist is free: a count per row and warp)
+  constexpr int kTurn = 8;
+  const u64 lk = sp.last_key;
+  const int la = sp.last_at;
   int done = 0;
-  for (int r0 = 0; r0 * kPickThreads < n; r0 += kHeld) {
-    unsigned bal[kHeld];
+  for (int r0 = 0; r0 * kThreads < n; r0 += kTurn) {
+    unsigned bal[kTurn];
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r) {
-      const int i = (r0 + r) * kPickThreads + tid;
+    for (int r = 0; r < kTurn; ++r) {
+      const int i = (r0 + r) * kThreads + tid;
       u64 k = 0;
-      if (i < n) k = r0 == 0 ? held[r] : keys[i];
+      if (i < n) k = kHeld >= kTurn && r0 == 0 ? held[r < kHeld ? r : 0] : keys[i];
       bal[r] = __ballot_sync(0xffffffffu, i < n && (k > lk || (k == lk && i <= la)));
-      if (lane == 0) hist[r * kPickWarps + warp] = __popc(bal[r]);
+      if (lane == 0) sp.hist[r * 32 + warp] = __popc(bal[r]);
     }
     __syncthreads();
-    if (warp < kHeld) {                          // warp r: the counts of row r become ranks within it
-      const int v = hist[warp * kPickWarps + lane];
+    for (int r = warp; r < kTurn; r += kWarps) {           // the counts of a row become ranks within it
+      const int v = lane < kWarps ? sp.hist[r * 32 + lane] : 0;
       int incl = v;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
         const int o = __shfl_up_sync(0xffffffffu, incl, off);
         if (lane >= off) incl += o;
       }
-      hist[warp * kPickWarps + lane] = incl - v;
-      if (lane == 31) cnt[warp] = incl;
+      sp.hist[r * 32 + lane] = incl - v;
+      if (lane == 31) sp.cnt[r] = incl;
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r) {
-      if (bal[r] >> lane & 1) out[a.sink + done + hist[r * kPickWarps + warp] + __popc(bal[r] & ((1u << lane) - 1))] = a.sink + (r0 + r) * kPickThreads + tid;
-      done += cnt[r];
+    for (int r = 0; r < kTurn; ++r) {
+      if (bal[r] >> lane & 1) out[done + sp.hist[r * 32 + warp] + __popc(bal[r] & ((1u << lane) - 1))] = first + (r0 + r) * kThreads + tid;
+      done += sp.cnt[r];
     }
     __syncthreads();
   }
 }
 
+template <int kPickThreads>
+__global__ void __launch_bounds__(kPickThreads) pick_kernel(const PagedView w, const SelectArgs a) {
+  __shared__ PickSpace<kPickThreads> sp;
+  begin();
+  const int b = blockIdx.y, h = blockIdx.x;
+  int32_t* out = nullptr;
+  const int n = pick_ends<kPickThreads>(w, a, b, h, out);
+  if (n == 0) return;
+  pick_largest<kPickThreads, 8>(a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages + a.sink, n, a.top, a.sink, out, sp);
+}
+
+constexpr int kSelectThreads = 256;
+constexpr int kSelectPages = 512;    // keys that a block keeps in shared memory at most
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kSelectThreads) select_kernel(const PagedView w, const SelectArgs a) {
+  extern __shared__ unsigned long long select_keys[];
+  __shared__ PickSpace<kSelectThreads> sp;
+  __shared__ double qsum[2 * D];
+  begin();
+  const int b = blockIdx.y, h = blockIdx.x;
+  int32_t* out = nullptr;
+  const int n = pick_ends<kSelectThreads>(w, a, b, h, out);
+  if (n == 0) return;
+  const int end = a.sink + n;
+  int lp0 = a.sink + (threadIdx.x & ~31);
+  int mine = look_up(w, a, b, lp0 + (threadIdx.x & 31), lp0 + (int)(threadIdx.x & 31) < end);
+  sum_queries<T, D, kSelectThreads>(a, w.kv_heads, b, h, qsum);
+  __syncthreads();
+  for (; lp0 < end; lp0 += kSelectThreads) {
+    const int next = lp0 + kSelectThreads + (threadIdx.x & 31);
+    const int then = look_up(w, a, b, next, next < end);              // under way while these pages are scored
+    score_pages<T, D>(w, h, lp0, end, mine, qsum, [&](int i, unsigned long long key) { select_keys[i - a.sink] = key; });
+    mine = then;
+  }
+  __syncthreads();
+  pick_largest<kSelectThreads, 0>(select_keys, n, a.top, a.sink, out, sp);
+}
+
 template <typename T, int D>
 cudaError_t launch(buzz_paged* c, int layer, const SelectArgs& a, cudaStream_t s) {
   const int middle = a.max_pages - a.sink - a.recent;
-  if (a.top > 0 && middle > a.top) {
-    const int per = ScorePlan<T, D>::kPerBlock;
-    const dim3 grid((middle + per - 1) / per, c->sh.kv_heads, a.batch);
+  const bool scored = a.top > 0 && middle > a.top;
+  // One block per (sequence, KV head) where there is little to read: a second launch costs more than the blocks that
+  // it would keep busy (8 against 11 us for up to 125 pages). With 256 such blocks of 512..1024 pages each it is
+  // slower (51 against 33 us), a block scores and then picks while nothing is under way.
+  if (scored && middle <= kSelectPages) {
+    const cudaError_t e = buzz_launch_chained(select_kernel<T, D>, dim3(c->sh.kv_heads, a.batch), (unsigned)kSelectThreads, middle * sizeof(unsigned long long),
+                                              s, c->view(layer), a);
+    if (e == cudaSuccess) c->launches += 1;
+    return e;
+  }
+  if (scored) {
+    const dim3 grid((middle + kScoreWarps * 32 - 1) / (kScoreWarps * 32), c->sh.kv_heads, a.batch);
     if (cudaError_t e = buzz_launch_chained(score_kernel<T, D>, grid, kScoreWarps * 32u, 0, s, c->view(layer), a); e != cudaSuccess) return e;
     c->launches += 1;
   }
-  const cudaError_t e = buzz_launch_chained(pick_kernel, dim3(c->sh.kv_heads, a.batch), (unsigned)kPickThreads, 0, s, c->view(layer), a);
+  // 2048 keys fit the registers of 256 threads, and more such blocks an SM
+  const dim3 picks(c->sh.kv_heads, a.batch);
+  const cudaError_t e = middle <= 2048 ? buzz_launch_chained(pick_kernel<256>, picks, 256u, 0, s, c->view(layer), a)
+                                       : buzz_launch_chained(pick_kernel<1024>, picks, 1024u, 0, s, c->view(layer), a);
   if (e == cudaSuccess) c->launches += 1;
   return e;
 }

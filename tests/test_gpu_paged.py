@@ -254,12 +254,20 @@ def test_decode_logn(cuda_device, dtype, kind):
     attend_case(dtype, kind, [1, 2, 100, 512, 1500], 32, 4, 2, 128, 5, logn=True)
 
 
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("lens", [[1024, 1, 0, 1000], [700, 2100], [1500] * 19])
+def test_decode_one_block_per_head_or_split(cuda_device, dtype, kind, lens):
+    """Lengths around the limit up to which a block does a (sequence, KV head) alone, and more heads than SMs."""
+    attend_case(dtype, kind, lens, 64, 16, 8, 128, len(lens))
+
+
 def test_decode_is_reproducible_and_ignores_a_loose_bound(cuda_device):
     pool, table, ks, vs, q, out = attend_case(BF16, BF16, [3000, 17, 1], 16, 8, 2, 128, 9)
     for _ in range(5):
         again = torch.empty_like(out)
         pool.decode(1, q.to(DEV), dev_lens([3000, 17, 1]), table.to(DEV), 3000, again)
         assert torch.equal(again, out)
+    again.fill_(3.0)
     pool.decode(1, q.to(DEV), dev_lens([3000, 17, 1]), table.to(DEV), table.shape[1] * 16, again)
     assert torch.equal(again, out)
 
@@ -392,6 +400,29 @@ def test_select_many_pages(cuda_device, top):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_select_ties_go_to_the_lowest_page(cuda_device, dtype):
     select_case(dtype, dtype, [1600, 800, 2000], 16, 2, 2, 64, 1, 1, 11, 13, tie=True)
+
+
+@pytest.mark.parametrize("pages,heads", [(500, 1), (900, 1), (9000, 2)])
+def test_select_many_equal_scores(cuda_device, pages, heads):
+    """A crowd at the border that is one value: the lowest of its pages are kept."""
+    n = 16 * pages
+    pool, table, _ = make(BF16, BF16, [n], 16, heads, heads, 64, gen(7))
+    b = torch.zeros(pages, heads, 2, 64, dtype=BF16)
+    b[100, :, 1, 0], b[pages - 7, :, 1, 0], b[3, :, 0, 0], b[3, :, 1, 0] = 1.0, 2.0, -1.0, -0.5
+    pool.bounds[0, table[0, :pages].long()] = b.to(DEV)
+    q = torch.zeros(1, heads, 64, dtype=BF16)
+    q[..., 0] = 1.0
+    for top in (1, 2, 3, 40, 300):
+        sel = torch.empty(1, heads, top + 2, dtype=torch.int32, device=DEV)
+        pool.select(0, q.to(DEV), dev_lens([n]), table.to(DEV), n, 1, 1, top, sel)
+        order = [pages - 7, 100] + [i for i in range(1, pages - 1) if i not in (3, 100, pages - 7)] + [3]
+        assert sel[0].tolist() == [[0] + sorted(order[:top]) + [pages - 1]] * heads, top
+    assert pool.status() == 0
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 128), (BF16, 64)])
+def test_select_with_many_heads(cuda_device, dtype, d):
+    select_case(dtype, dtype, [11000, 3, 9999, 400, 700], 16, 32, 32, d, 1, 3, 50, d)
 
 
 def test_select_special_scores(cuda_device):
