@@ -170,7 +170,8 @@ constexpr int kRanked = 256;         // keys that are ranked directly
 template <int kThreads>
 struct PickSpace {
   int hist[kBins];
-  unsigned long long ends[2][kThreads / 32], cand[kRanked], last_key;
+  unsigned long long cand[kRanked], last_key;
+  uint32_t ends[2][kThreads / 32];
   int cand_at[kRanked], cnt[32], border, border_rest, border_count, cand_n, last_at;
 };
 
@@ -204,7 +205,7 @@ __device__ __forceinline__ void pick_largest(const unsigned long long* keys, int
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
   // key i of the thread is that of page i * kThreads + tid; the first kHeld are kept in registers
   u64 held[kHeld > 0 ? kHeld : 1];
-  u64 small = ~0ull, large = 0;
+  uint32_t small = ~0u, large = 0;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) held[i] = i * kThreads + tid < n ? keys[i * kThreads + tid] : 0;
   auto each = [&](auto&& f) {
@@ -213,29 +214,21 @@ __device__ __forceinline__ void pick_largest(const unsigned long long* keys, int
       if (i * kThreads + tid < n) f(held[i], i * kThreads + tid);
     for (int i = kHeld * kThreads + tid; i < n; i += kThreads) f(keys[i], i);
   };
-  each([&](u64 k, int) { small = min(small, k); large = max(large, k); });
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    small = min(small, __shfl_xor_sync(0xffffffffu, small, off));
-    large = max(large, __shfl_xor_sync(0xffffffffu, large, off));
-  }
+  // The first histograms go by the upper halves of the keys (sign, exponent and 20 bits of the score), 32-bit
+  // arithmetic for what takes twice to three times as much in 64; the lower halves are looked at only where more
+  // keys than can be ranked have one upper half.
+  each([&](u64 k, int) { const uint32_t u = (uint32_t)(k >> 32); small = min(small, u); large = max(large, u); });
+  small = __reduce_min_sync(0xffffffffu, small);
+  large = __reduce_max_sync(0xffffffffu, large);
   if (lane == 0) { sp.ends[0][warp] = small; sp.ends[1][warp] = large; }
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) sp.hist[i * kThreads + tid] = 0;
   if (tid == 0) sp.cand_n = 0;
   __syncthreads();
-  small = sp.ends[0][lane % kWarps];
-  large = sp.ends[1][lane % kWarps];
-#pragma unroll
-  for (int off = kWarps / 2; off > 0; off >>= 1) {
-    small = min(small, __shfl_xor_sync(0xffffffffu, small, off));
-    large = max(large, __shfl_xor_sync(0xffffffffu, large, off));
-  }
-  u64 base = small, span = large - small;        // keys base .. base + span hold the border
-  int rest = top, shift;                         // how many of them are kept
-  for (;;) {
-    shift = max(0, 64 - __clzll((long long)span) - 11);
-    each([&](u64 k, int) { if (k - base <= span) atomicAdd(&sp.hist[(int)((k - base) >> shift)], 1); });
+  small = __reduce_min_sync(0xffffffffu, sp.ends[0][lane % kWarps]);
+  large = __reduce_max_sync(0xffffffffu, sp.ends[1][lane % kWarps]);
+  // of the histogram, the bin in which the border lies, and what is left to keep of it
+  auto find_border = [&](int rest) {
     __syncthreads();
     // bins from the top: thread t has kOwn of them, from kBins - 1 - kOwn t downwards
     int c[kOwn], sum = 0;
@@ -261,10 +254,33 @@ __device__ __forceinline__ void pick_largest(const unsigned long long* keys, int
       over += c[i];
     }
     __syncthreads();
+  };
+  int rest = top;                                // how many of the keys in reach of the border are kept
+  u64 base, span;                                // those keys are base .. base + span
+  {
+    uint32_t low = small, reach = large - small;
+    for (;;) {
+      const int shift = max(0, 32 - __clz((int)reach) - 11);
+      each([&](u64 k, int) {
+        const uint32_t u = (uint32_t)(k >> 32) - low;
+        if (u <= reach) atomicAdd(&sp.hist[u >> shift], 1);
+      });
+      find_border(rest);
+      low += (uint32_t)sp.border << shift;
+      reach = (1u << shift) - 1;
+      rest = sp.border_rest;
+      if (sp.border_count <= kRanked || shift == 0) break;
+    }
+    base = (u64)low << 32;
+    span = ((u64)reach << 32) | 0xffffffffu;
+  }
+  while (sp.border_count > kRanked && span > 0) {  // one upper half so far
+    const int shift = max(0, 64 - __clzll((long long)span) - 11);
+    each([&](u64 k, int) { if (k - base <= span) atomicAdd(&sp.hist[(int)((k - base) >> shift)], 1); });
+    find_border(rest);
     base += (u64)sp.border << shift;
     span = (1ull << shift) - 1;
     rest = sp.border_rest;
-    if (sp.border_count <= kRanked || shift == 0) break;
   }
   // the last key that is kept: the one of rank `rest` in the border's bin
   const int crowd = sp.border_count;
