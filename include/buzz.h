@@ -329,7 +329,9 @@ int buzz_norm_rope(const buzz_rope_shape* shape, const void* q, const void* k, c
  * The library never reads the device arrays on the host. On the device, a length outside [0, bound] or
  * a page outside the pool records BUZZ_ERR_INVALID at buzz_paged_status(): such a sequence is skipped
  * and its rows are left as they were; of a bad page the tokens are skipped and take no part.
- * A sequence of length 0 attends to nothing: output 0, log-sum-exp -infinity. */
+ * A sequence of length 0 attends to nothing: output 0, log-sum-exp -infinity.
+ * A wait for memory that runs out records BUZZ_ERR_TIMEOUT there (it never does in a correct build).
+ * No output may overlap an input or the pool. */
 enum { BUZZ_E4M3 = 2, BUZZ_I8 = 3 };
 
 typedef struct buzz_paged* buzz_paged_t;
@@ -361,10 +363,11 @@ int buzz_paged_create(buzz_paged_t* out, const buzz_paged_shape* shape, const bu
 void buzz_paged_destroy(buzz_paged_t ctx);
 
 /* Writes new rows k, v [total_tokens][Hkv][d], packed over `batch` sequences by cu_seqlens_dev
- * [batch+1] (NULL: one token per sequence, total_tokens = batch). The tokens of sequence b become its
- * last ones, positions lens[b] - new .. lens[b] - 1. Where the pool has bounds, a page's bounds are
- * widened, or begun where its first slot is written; a NaN does not count in them. `max_new` is an
- * upper bound on the new tokens of a sequence. No page may be written through two sequences at once.
+ * [batch+1] (NULL: one token per sequence, total_tokens = batch); rows from cu_seqlens_dev[batch] on are
+ * not read. The tokens of sequence b become its last ones, positions lens[b] - new .. lens[b] - 1. Where
+ * the pool has bounds, a page's bounds are widened, or begun where its first slot is written; a NaN does
+ * not count in them, and shortening a sequence does not narrow them. `max_new` is an upper bound on the
+ * new tokens of a sequence. No page may be written through two sequences at once.
  * Rejects: layer or batch out of range (batch 1..65535), total_tokens < 1, max_new < 1 or > total_tokens,
  * table_stride < 1, null or misaligned pointers. */
 int buzz_paged_append(buzz_paged_t ctx, int layer, const void* k, const void* v, const int32_t* cu_seqlens_dev,
@@ -372,13 +375,15 @@ int buzz_paged_append(buzz_paged_t ctx, int layer, const void* k, const void* v,
                       const int32_t* table_dev, int table_stride, void* stream);
 
 /* The inverse: copies the last tokens of each sequence (counts from cu_seqlens_dev, as above) out of
- * the pages to k_out, v_out [total_tokens][Hkv][d], scaled back and rounded to `dtype`. */
+ * the pages to k_out, v_out [total_tokens][Hkv][d], scaled back and rounded to `dtype`; rows from
+ * cu_seqlens_dev[batch] on are left as they were. */
 int buzz_paged_read(buzz_paged_t ctx, int layer, void* k_out, void* v_out, const int32_t* cu_seqlens_dev,
                     int batch, int total_tokens, int max_new, const int32_t* lens_dev,
                     const int32_t* table_dev, int table_stride, void* stream);
 
 /* Workspace that one buzz_paged_decode and one buzz_paged_select call of this size need. It holds
- * nothing between calls; calls that may run at the same time need one each. */
+ * nothing between calls; calls that may run at the same time need one each. Where 0 bytes are needed the
+ * call takes NULL. */
 int buzz_paged_workspace_bytes(buzz_paged_t ctx, int batch, int max_len, size_t* decode_bytes,
                                size_t* select_bytes);
 
@@ -387,10 +392,11 @@ int buzz_paged_workspace_bytes(buzz_paged_t ctx, int batch, int max_len, size_t*
  * of the sum of the exponentials of the logits, by which results over disjoint tokens can be joined.
  * The new token's own row is attended to if it has been appended before.
  * `selected` (or NULL: all pages) int32 [batch][Hkv][selected_stride] lists the logical pages to attend
- * to, per KV head: the first min(pages of the sequence, selected_stride) entries, each page once, in
- * any order; an entry outside the sequence's pages is treated as a bad page.
+ * to, per KV head: the first min(pages of the sequence, selected_stride) entries, in any order; an entry
+ * outside the sequence's pages is treated as a bad page, a page listed twice counts twice.
  * Split over the length where there are few sequences, and joined in a fixed order: results do not
- * depend on timing. */
+ * depend on timing. Keys or queries of fp32 that are not finite, or beyond 3.38e38, give NaN: they are
+ * multiplied in parts. */
 int buzz_paged_decode(buzz_paged_t ctx, int layer, const void* q, const int32_t* lens_dev,
                       const int32_t* table_dev, int table_stride, int batch, int max_len,
                       const int32_t* selected, int selected_stride, void* out, float* lse,

@@ -363,13 +363,16 @@ def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps=1e
               stream=None):
     """buzz_norm_rope: RMS norm of every head of q [T, Hq, d] and k [T, Hkv, d] (where its weight [d] is given) and
     rotation by `positions` (int32 [T]) at `inv_freq` (fp32 [rotary_dim / 2]). q and k may be slices of one
-    projection's output. Returns (q_out, k_out), made here unless given; an output may be its input."""
+    projection's output. Returns (q_out, k_out), made here (for the call's stream) unless given; an output may be its
+    input."""
     device, dtype = q.device, q.dtype
     _need(q.dim() == 3 and k.dim() == 3, "q and k: [tokens, heads, d]")
     if device.type != "cuda":
         raise ValueError(f"q: on {device}; there is no CPU fallback")
     if dtype not in _DTYPES:
         raise ValueError(f"q: {dtype} is not supported")
+    if (q.requires_grad or k.requires_grad) and torch.is_grad_enabled():
+        raise ValueError("q and k: the rotation has no backward pass; detach them or call under torch.no_grad()")
     T, Hq, d = q.shape
     Hk = k.shape[1]
     pos, freq = _tensor("positions", positions, device, torch.int32, (T,)), _tensor("inv_freq", inv_freq, device, torch.float32, (None,))
@@ -378,11 +381,11 @@ def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps=1e
     qs, ks = _token_stride("q", q, device, dtype, T, Hq, d), _token_stride("k", k, device, dtype, T, Hk, d)
     with _On(device, stream) as s:
         if q_out is None:
-            q_out, qos = torch.empty((T, Hq, d), dtype=dtype, device=device), Hq * d
+            q_out, qos = torch.empty_like(q, memory_format=torch.contiguous_format), Hq * d
         else:
             qos = _token_stride("q_out", q_out, device, dtype, T, Hq, d)
         if k_out is None:
-            k_out, kos = torch.empty((T, Hk, d), dtype=dtype, device=device), Hk * d
+            k_out, kos = torch.empty_like(k, memory_format=torch.contiguous_format), Hk * d
         else:
             kos = _token_stride("k_out", k_out, device, dtype, T, Hk, d)
         sh = _RopeShape(Hq, Hk, d, 2 * inv_freq.shape[0], _DTYPES[dtype], 1 if interleaved else 0, eps, 0, qs, ks, qos, kos)
@@ -507,9 +510,10 @@ class BuzzPaged:
         qp = _tensor("q", q, self.device, self.dtype, (batch, self.q_heads, self.head_dim))
         sp = _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, sink + recent + top))
         with _On(self.device, stream) as s:
-            n = max(16, self._scratch_bytes(batch, max_len)[1])
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            _check(self._lib.buzz_paged_select(self._h, layer, qp, lp, tp, stride, batch, max_len, sink, recent, top, sp, ws.data_ptr(), n, s),
+            n = self._scratch_bytes(batch, max_len)[1]
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+            _check(self._lib.buzz_paged_select(self._h, layer, qp, lp, tp, stride, batch, max_len, sink, recent, top, sp,
+                                               None if ws is None else ws.data_ptr(), n, s),
                    "buzz_paged_select")
 
     def status(self, stream=None) -> int:

@@ -421,6 +421,7 @@ size_t buzz_paged_decode_workspace(const buzz_paged* c);
 
 static size_t select_workspace(const buzz_paged* c, int batch, int max_len) {
   const size_t pages = ((size_t)max_len + c->sh.page_tokens - 1) / c->sh.page_tokens;
+  if (pages <= kSelectPages) return 0;             // select_kernel keeps its keys in shared memory
   return (size_t)batch * c->sh.kv_heads * pages * sizeof(unsigned long long);
 }
 
@@ -437,11 +438,12 @@ extern "C" int buzz_paged_select(buzz_paged_t c, int layer, const void* q, const
   if (!c || !c->buf.bounds || layer < 0 || layer >= c->sh.layers || batch < 1 || batch > 65535 || table_stride < 1) return BUZZ_ERR_INVALID;
   if (max_len < 0 || max_len > (int64_t)table_stride * c->sh.page_tokens) return BUZZ_ERR_INVALID;
   if (sink < 0 || recent < 1 || top < 0 || (int64_t)sink + recent + top > 32768) return BUZZ_ERR_INVALID;
-  if (!q || !lens_dev || !table_dev || !selected || !workspace) return BUZZ_ERR_INVALID;
+  const size_t need = select_workspace(c, batch, max_len);
+  if (!q || !lens_dev || !table_dev || !selected || (need > 0 && !workspace)) return BUZZ_ERR_INVALID;
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(workspace)) & 15u) return BUZZ_ERR_INVALID;
   if ((reinterpret_cast<uintptr_t>(lens_dev) | reinterpret_cast<uintptr_t>(table_dev) | reinterpret_cast<uintptr_t>(selected)) & 3u)
     return BUZZ_ERR_INVALID;
-  if (workspace_bytes < select_workspace(c, batch, max_len)) return BUZZ_ERR_INVALID;
+  if (workspace_bytes < need) return BUZZ_ERR_INVALID;
   SelectArgs a;
   a.q = q; a.lens = lens_dev; a.table = table_dev;
   a.keys = static_cast<unsigned long long*>(workspace);

@@ -476,6 +476,49 @@ def test_select_bad_lengths_and_pages(cuda_device):
     assert torch.equal(out[0], want[0]) and bool((out[1] == 0).all())
 
 
+def test_a_page_listed_twice_counts_twice(cuda_device):
+    pool, table, ks, vs, q, out = attend_case(BF16, I8, [60], 16, 2, 1, 64, 65)
+    pool.decode(1, q.to(DEV), dev_lens([60]), table.to(DEV), 60, out, selected=torch.tensor([[[3, 1, 1]]], dtype=torch.int32, device=DEV))
+    assert pool.status() == 0
+    rows = list(range(48, 60)) + list(range(16, 32)) * 2
+    o, _, ob, _ = ref.attention(q[0], kept(ks[0][rows], I8).transpose(0, 1), kept(vs[0][rows], I8).transpose(0, 1), BF16)
+    within(out[0], o, ob)
+
+
+def test_rows_behind_the_last_sequence(cuda_device):
+    """Packed rows that belong to no sequence are neither read nor written."""
+    g = gen(66)
+    pool, table, _ = make(BF16, E4M3, [20, 5], 16, 2, 2, 64, g)
+    x = torch.randn(40, 2, 64, generator=g).to(BF16)
+    x[25:] = math.nan
+    cu, lens, t = cu_of([20, 5]).to(DEV), dev_lens([20, 5]), table.to(DEV)
+    pool.append(0, x.to(DEV), x.to(DEV), lens, t, cu, 20)
+    ko, vo = [torch.full((40, 2, 64), 3.0, dtype=BF16, device=DEV) for _ in range(2)]
+    pool.read(0, lens, t, ko, vo, cu, 20)
+    assert pool.status() == 0
+    for y in (ko, vo):
+        assert torch.equal(y[:25].cpu(), kept(x[:25], E4M3).to(BF16)) and bool((y[25:] == 3.0).all())
+
+
+def test_everything_on_a_stream_of_its_own(cuda_device):
+    g = gen(67)
+    want_pool, table, ks, vs, q, want = attend_case(BF16, E4M3, [900, 30], 16, 4, 2, 64, 68)
+    pool, table, _ = make(BF16, E4M3, [900, 30], 16, 4, 2, 64, g)
+    k, v, lens, t, cu, qd = pack(ks, 2, 64).to(DEV), pack(vs, 2, 64).to(DEV), dev_lens([900, 30]), table.to(DEV), cu_of([900, 30]).to(DEV), q.to(DEV)
+    out, all_pages = torch.empty_like(want), torch.empty_like(want)
+    sel = torch.empty(2, 2, 57, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    pool.append(0, k, v, lens, t, cu, 900, stream=side)
+    pool.decode(0, qd, lens, t, 900, out, stream=side)
+    pool.select(0, qd, lens, t, 900, 1, 1, 55, sel, stream=side)
+    pool.decode(0, qd, lens, t, 900, all_pages, selected=sel, stream=side)
+    assert pool.status(side) == 0
+    assert torch.equal(out, want) and torch.equal(all_pages, want)
+    with pytest.raises(ValueError):
+        norm_rope(qd.float().requires_grad_(), qd.float(), torch.zeros(2, dtype=torch.int32, device=DEV), torch.ones(8, device=DEV))
+
+
 # ---- arguments -----------------------------------------------------------------------------------
 
 def test_refusals(cuda_device):
@@ -508,8 +551,9 @@ def test_refusals(cuda_device):
     assert lib.buzz_paged_workspace_bytes(h, 0, 1, ctypes.byref(n), ctypes.byref(n)) == -1
     assert lib.buzz_paged_decode(h, 0, q.data_ptr(), lens.data_ptr(), t.data_ptr(), t.shape[1], 2, 40, None, 0, out.data_ptr(), None,
                                  x.data_ptr(), 8, None) == -1                      # a workspace that is too small
-    assert lib.buzz_paged_select(h, 0, q.data_ptr(), lens.data_ptr(), t.data_ptr(), t.shape[1], 2, 40, 1, 1, 1, sel.data_ptr(),
-                                 x.data_ptr(), 8, None) == -1
+    wide = torch.zeros(2, 600, dtype=torch.int32, device=DEV)
+    for ws in (None, x.data_ptr()):                           # no workspace, and one that is too small
+        assert lib.buzz_paged_select(h, 0, q.data_ptr(), lens.data_ptr(), wide.data_ptr(), 600, 2, 9600, 1, 1, 1, sel.data_ptr(), ws, 8, None) == -1
     assert pool.launch_count() == before
     bare, table, _ = make(BF16, BF16, [40, 30], 16, 4, 2, 64, gen(72), bounds=False)
     with pytest.raises(ValueError):
