@@ -30,6 +30,8 @@
 //                stay exact down to 2^-28 of it; fp32 queries are two parts). The values' row scales go
 //                into the probabilities, relative to the largest scale met so far and times 2^14, in two
 //                parts; outputs are rescaled when that largest one grows, as they are for the maximum.
+#include <cooperative_groups.h>
+
 #include <type_traits>
 
 #include "paged_internal.cuh"
@@ -37,11 +39,11 @@
 
 namespace {
 
+namespace cg = cooperative_groups;
 using namespace buzz_paged_dev;
 
 constexpr int kHeads = 8;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr long long kWholeBytes = 512 << 10;
 constexpr float kSlack = 6.f;        // log2 of the largest probability before the maximum in use is raised
 constexpr float kUnit = 256.f;       // 8-bit caches: weight of a probability of 1 at the largest value scale; times 2^kSlack and 2, below 2^16
 
@@ -51,7 +53,7 @@ struct DecodeArgs {
   float* lse;
   const int32_t *lens, *table, *selected;
   int table_stride, selected_stride, batch, max_len, group, logn;
-  int whole;       // a block per (sequence, KV head): nothing is split, nothing joined
+  int share;       // 0: blocks take stretches of the line; n: a cluster of n blocks per (sequence, KV head)
   float scale_log2;
   int4* desc;      // [blocks]: (instance whose join this block begins, or -1; last block of it)
   float* part;     // [blocks][2][part_floats]: outputs [group][D], maxima [8], sums [8]
@@ -90,7 +92,7 @@ struct Plan {
   static constexpr int kBars = kScales + (C::kScaled ? kRing * 2 * kTok * 4 : 0);
   static constexpr int kMerge = kBars + (kRing * (8 + 4) + 15) / 16 * 16;
   static size_t smem(int group) {
-    return 1024 + (size_t)kMerge + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads + kHeads);
+    return 1024 + (size_t)kMerge + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads + 2 * kHeads);
   }
 };
 
@@ -245,6 +247,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   float* wm = obuf + kSlots * a.group * D;       // [warps][8] maxima
   float* wl = wm + kWarps * kHeads;              // [warps][8] sums, over the largest maximum
   float* wt = wl + kWarps * kHeads;              // [8] largest maxima
+  float* ws = wt + kHeads;                       // [8] sums of the block, where a cluster shares a head
   __shared__ long long warp_sum[kThreads / 32];
   __shared__ int found[2];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
@@ -260,14 +263,17 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   Place cur;
   int n = 0, n_units;
   long long U = 0, u_begin = 0;
-  if (a.whole) {
-    cur.b = blockIdx.x / w.kv_heads;
-    cur.h = blockIdx.x - cur.b * w.kv_heads;
-    cur.unit = cur.next = 0;
+  const int rank = a.share > 1 ? blockIdx.x % a.share : 0;
+  if (a.share) {
+    const int head = blockIdx.x / a.share;
+    cur.b = head / w.kv_heads;
+    cur.h = head - cur.b * w.kv_heads;
+    cur.next = 0;
     const int len = a.lens[cur.b];
     set_sequence<L>(a, w, cur, len);
-    if (cur.bad && cur.h == 0 && tid == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, cur.b, len);
-    n_units = cur.units;
+    if (cur.bad && cur.h == 0 && rank == 0 && tid == 0) buzz_set_status(w.status, BUZZ_ERR_INVALID, cur.b, len);
+    cur.unit = (int)((long long)cur.units * rank / a.share);
+    n_units = (int)((long long)cur.units * (rank + 1) / a.share) - cur.unit;
     __syncthreads();
   } else {
     long long mine = 0;
@@ -728,7 +734,10 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
           const float4 v = *reinterpret_cast<const float4*>(obuf + i * a.group * D + 4 * x);
           o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
         }
-        if (whole) {
+        if (a.share > 1) {                         // for the cluster: in place of the first warps' outputs
+          *reinterpret_cast<float4*>(obuf + 4 * x) = o;
+          if (x % (D / 4) == 0) ws[hd] = sum;
+        } else if (whole) {
           if (!cur.bad) {
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             store4(static_cast<T*>(a.out) + head0 * D + 4 * x, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
@@ -739,7 +748,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
           if (x % (D / 4) == 0) { part[a.group * D + hd] = wt[hd]; part[a.group * D + kHeads + hd] = sum; }
         }
       }
-      if (u + 1 == n_units && tid == 0 && !a.whole) {
+      if (u + 1 == n_units && tid == 0 && !a.share) {
         // the join of an instance is described where the instance begins
         int4 d = make_int4(-1, 0, 0, 0);
         if (!complete && first_part) {
@@ -753,6 +762,36 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
     }
     if (u + 1 < n_units) advance<L>(a, w, cur, 1);
   }
+  if (a.share <= 1) return;
+
+  // ---- the cluster's parts, joined through its blocks' shared memory -------------------------------
+  cg::cluster_group cluster = cg::this_cluster();
+  if (n_units == 0 && tid < kHeads) {            // a short sequence leaves blocks without work
+    wt[tid] = -INFINITY;
+    ws[tid] = 0.f;
+  }
+  cluster.sync();
+  const size_t head0 = ((size_t)cur.b * w.kv_heads + cur.h) * a.group;
+  for (int x = rank * kThreads + tid; x < a.group * D / 4; x += a.share * kThreads) {
+    const int hd = x / (D / 4);
+    float most = -INFINITY, sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int r = 0; r < a.share; ++r) most = fmaxf(most, cluster.map_shared_rank(wt, r)[hd]);
+    for (int r = 0; r < a.share; ++r) {
+      const float mr = cluster.map_shared_rank(wt, r)[hd];
+      if (mr == -INFINITY) continue;             // nothing there
+      const float f = exp2f(mr - most);
+      const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(obuf, r) + 4 * x);
+      sum += cluster.map_shared_rank(ws, r)[hd] * f;
+      o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+    }
+    if (!cur.bad) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      store4(static_cast<T*>(a.out) + head0 * D + 4 * x, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+      if (a.lse && x % (D / 4) == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (most + log2f(sum)) * 0.69314718055994531f;
+    }
+  }
+  cluster.sync();                                // the others' shared memory is read until here
 }
 
 // Joins the parts of the (sequence, KV head) that begins in block blockIdx.x and ends in a later one: the
@@ -827,19 +866,25 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
   }
   const long long units = (tokens + L::kTok * L::kWarps - 1) / (L::kTok * L::kWarps);          // of a (sequence, KV head), at most
   const long long all = (long long)a.batch * c->sh.kv_heads * (units > 0 ? units : 1);
-  // Where a block could do each (sequence, KV head) alone, the join (a launch, 4 us on the host and 3 on the GPU) is
-  // not worth it: up to half a megabyte, which one SM reads in 4 us, and no more of them than SMs.
+  // Few (sequence, KV head)s and little to read: each gets a cluster of 1 to 8 blocks of its own, which join their
+  // parts in shared memory; the join through global memory is a second launch (4 us on the host, 3 to 4 on the
+  // GPU). As many blocks as there are units, as clusters find SMs (128 blocks), and only while a block reads four
+  // units or fewer: from there on the even cut over all SMs is faster (one sequence, 8 KV heads, bf16, d = 128:
+  // see below).
   const long long heads = (long long)a.batch * c->sh.kv_heads;
-  a.whole = units * L::kWarps * 2 * L::kTileBytes <= kWholeBytes && heads <= c->sm_count;
-  const int n = (int)(a.whole ? heads : all < c->sm_count ? all : c->sm_count);
+  int share = 1;
+  while (share < 8 && share < units && heads * share * 2 <= 128) share *= 2;
+  a.share = heads <= c->sm_count && (units + share - 1) / share <= 4 ? share : 0;
+  const int n = (int)(a.share ? heads * share : all < c->sm_count ? all : c->sm_count);
   const size_t smem = L::smem(c->group);
   static BuzzSmemOptIn opt_in;
   if (cudaError_t e = opt_in.ensure(paged_decode_kernel<T, C, D>, smem); e != cudaSuccess) return e;
-  if (cudaError_t e = buzz_launch_chained(paged_decode_kernel<T, C, D>, dim3(n), L::kThreads, smem, stream, c->view(layer), a, c->k_map, c->v_map);
+  if (cudaError_t e = buzz_launch_chained_cluster(paged_decode_kernel<T, C, D>, dim3(n), L::kThreads, smem, stream, a.share, c->view(layer), a,
+                                                  c->k_map, c->v_map);
       e != cudaSuccess)
     return e;
   c->launches += 1;
-  if (units <= 1 || a.whole) return cudaSuccess;   // nothing is split
+  if (units <= 1 || a.share) return cudaSuccess;   // nothing is split, or joined already
   cudaError_t e = buzz_launch_chained(paged_join_kernel<T, D>, dim3(n), (unsigned)kJoinThreads, sizeof(float) * c->group * n, stream, a);
   if (e == cudaSuccess) c->launches += 1;
   return e;

@@ -71,18 +71,26 @@ struct CacheI8 { static constexpr int kSize = 1; static constexpr bool kScaled =
 // that kernel's end: the launch latency is hidden, the order of the stream is kept. The wait is made by
 // every block of every such kernel, so that the end of one implies the end of all before it.
 template <typename... P, typename... A>
-inline cudaError_t buzz_launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const A&... args) {
+inline cudaError_t buzz_launch_chained_cluster(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, int cluster,
+                                               const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename... P, typename... A>
+inline cudaError_t buzz_launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const A&... args) {
+  return buzz_launch_chained_cluster(kernel, grid, threads, smem, stream, 1, args...);
 }
 
 namespace buzz_paged_dev {
