@@ -867,14 +867,18 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
   const long long units = (tokens + L::kTok * L::kWarps - 1) / (L::kTok * L::kWarps);          // of a (sequence, KV head), at most
   const long long all = (long long)a.batch * c->sh.kv_heads * (units > 0 ? units : 1);
   // Few (sequence, KV head)s and little to read: each gets a cluster of 1 to 8 blocks of its own, which join their
-  // parts in shared memory; the join through global memory is a second launch (4 us on the host, 3 to 4 on the
-  // GPU). As many blocks as there are units, as clusters find SMs (128 blocks), and only while a block reads four
-  // units or fewer: from there on the even cut over all SMs is faster (one sequence, 8 KV heads, bf16, d = 128:
-  // see below).
+  // parts in shared memory. The join through global memory is a second launch (4 us on the host) and takes the
+  // GPU 3 us longer, the time of two units, so the cluster is taken while a block of it reads at most two units
+  // more than an even cut over all SMs gives it. Measured, bf16, d = 128, us for the cluster and for the cut: 8
+  // heads x 1024 tokens 7.8, 9.5; 32 x 2048 11.0, 13.5; 128 x 1024 14.9, 18.5; 8 x 4096 11.8, 11.7; 72 x 1024
+  // 14.9, 14.8; 72 x 2048 25.2, 20.2. Eight units at most, since lengths may differ. Sixteen clusters of eight
+  // do not find SMs at once (16 heads x 517 tokens: 14.0 us, with clusters of four 8.7): four from 9 heads on,
+  // two from 33 on.
   const long long heads = (long long)a.batch * c->sh.kv_heads;
-  int share = 1;
-  while (share < 8 && share < units && heads * share * 2 <= 128) share *= 2;
-  a.share = heads <= c->sm_count && (units + share - 1) / share <= 4 ? share : 0;
+  int share = heads <= 8 ? 8 : heads <= 32 ? 4 : heads <= 64 ? 2 : 1;
+  while (share > 1 && share / 2 >= units) share /= 2;
+  const long long each = (units + share - 1) / share, even = (units * heads + c->sm_count - 1) / c->sm_count;
+  a.share = heads <= c->sm_count && each <= 8 && each <= even + 2 ? share : 0;
   const int n = (int)(a.share ? heads * share : all < c->sm_count ? all : c->sm_count);
   const size_t smem = L::smem(c->group);
   static BuzzSmemOptIn opt_in;
