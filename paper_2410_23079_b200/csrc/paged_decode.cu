@@ -43,6 +43,7 @@ namespace cg = cooperative_groups;
 using namespace buzz_paged_dev;
 
 constexpr int kHeads = 8;
+constexpr int kPad = 8;            // floats between the heads of a block's outputs, see dim_of()
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 6.f;        // log2 of the largest probability before the maximum in use is raised
 constexpr float kUnit = 256.f;       // 8-bit caches: weight of a probability of 1 at the largest value scale; times 2^kSlack and 2, below 2^16
@@ -84,6 +85,7 @@ struct Plan {
   static constexpr int kQ = sizeof(T) == 2 ? 1 : kHalf ? 2 : 3;    // parts of a query, of a probability, of a cached value
   static constexpr int kP = kHalf || sizeof(T) == 2 ? 2 : 3;
   static constexpr int kC = C::kSize == 4 ? 3 : 1;
+  static constexpr int kVE = kChunks >= 8 ? kE : D / 8;            // consecutive dims of a lane's value chunk
   static constexpr bool kOffset = sizeof(T) == 2 && C::kScaled && std::is_same<C, CacheI8>::value;   // keys of int8 keep their offset of 1152
   static_assert(kStages >= 2, "a ring holds two tiles at least");
   static_assert(kBox == 128 || kBox == 64, "swizzles of 128 and 64 bytes");
@@ -92,7 +94,7 @@ struct Plan {
   static constexpr int kBars = kScales + (C::kScaled ? kRing * 2 * kTok * 4 : 0);
   static constexpr int kMerge = kBars + (kRing * (8 + 4) + 15) / 16 * 16;
   static size_t smem(int group) {
-    return 1024 + (size_t)kMerge + sizeof(float) * ((size_t)kSlots * group * D + 2 * kWarps * kHeads + 2 * kHeads);
+    return 1024 + (size_t)kMerge + sizeof(float) * ((size_t)kSlots * group * (D + kPad) + 2 * kWarps * kHeads + 2 * kHeads);
   }
 };
 
@@ -171,6 +173,20 @@ __device__ __forceinline__ void chunk_to_words(const uint4& u, uint32_t (&w)[kC]
   }
 }
 
+// Outputs under way to their place are kept in the order in which lanes hold them: product i, lane row g, two dims
+// that differ by one. Stores of a warp then meet all banks (with kPad between heads); in the order of the dims
+// 16 lanes met one bank, and a merge took 1.7 us. Pair y of a head, in that order, is dims dim_of(y), dim_of(y) + 1.
+template <int kVE>
+__device__ __forceinline__ int dim_of(int y) {
+  const int i = y >> 3, g = y & 7;
+  return (g + 8 * (i / (kVE / 2))) * kVE + 2 * (i % (kVE / 2));
+}
+template <typename T>
+__device__ __forceinline__ void store2(T* p, float x, float y) {
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(p) = pack_bf16(x, y);
+  else *reinterpret_cast<float2*>(p) = make_float2(x, y);
+}
+
 // Four consecutive elements.
 template <typename T>
 __device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
@@ -182,12 +198,6 @@ __device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
     x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
   }
 }
-template <typename T>
-__device__ __forceinline__ void store4(T* p, float4 x) {
-  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-  else *reinterpret_cast<float4*>(p) = x;
-}
-
 // A place on the line of work.
 struct Place {
   int b, h, unit;       // sequence, KV head, unit within (b, h)
@@ -235,7 +245,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   constexpr int kMK = kE / 4;                    // products per chunk of K
   constexpr int kKL = kChunks / 4;               // chunks per lane and key row
   constexpr int kVJ = kChunks >= 8 ? kChunks / 8 : 1;
-  constexpr int kVE = D / 8 / kVJ;               // elements per lane, value row and j
+  constexpr int kVE = L::kVE;                    // elements per lane, value row and j
   constexpr int kOut = D / 16;                   // products per 16 rows of V
 
   extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -243,8 +253,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   float* scales = reinterpret_cast<float*>(smem + L::kScales);                   // [ring][2][kTok]
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);                 // [warps][stages]
   uint32_t* counts = reinterpret_cast<uint32_t*>(full + L::kRing);              // valid rows of each 16-row part, a byte each
-  float* obuf = reinterpret_cast<float*>(smem + L::kMerge);                      // [slots][group][D]
-  float* wm = obuf + kSlots * a.group * D;       // [warps][8] maxima
+  float* obuf = reinterpret_cast<float*>(smem + L::kMerge);                      // [slots][group][D + kPad], see dim_of()
+  float* wm = obuf + kSlots * a.group * (D + kPad);       // [warps][8] maxima
   float* wl = wm + kWarps * kHeads;              // [warps][8] sums, over the largest maximum
   float* wt = wl + kWarps * kHeads;              // [8] largest maxima
   float* ws = wt + kHeads;                       // [8] sums of the block, where a cluster shares a head
@@ -383,7 +393,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
     return rows;
   };
   Place p = cur;
-  if (lane > 0) advance<L>(a, w, p, lane);
+  if (lane > 0 && lane < n_units) advance<L>(a, w, p, lane);
   Look now, next;
   look_logical(now, p, lane < n_units);
   if (lane + 32 < n_units) advance<L>(a, w, p, 32);
@@ -710,9 +720,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               if (2 * t + e >= a.group) continue;
-              const int j = i / (kVE / 2), k = i % (kVE / 2);
-              const int dim = (kChunks >= 8 ? (g + 8 * j) * kE : g * kVE) + 2 * k;
-              float2* o = reinterpret_cast<float2*>(obuf + ((warp % kSlots) * a.group + 2 * t + e) * D + dim);
+              float2* o = reinterpret_cast<float2*>(obuf + ((warp % kSlots) * a.group + 2 * t + e) * (D + kPad)) + i * 8 + g;
               float2 v = make_float2(oc[i][e] * f[e], oc[i][2 + e] * f[e]);
               if (round > 0) { const float2 old = *o; v.x += old.x; v.y += old.y; }
               *o = v;
@@ -723,29 +731,30 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
       const bool whole = complete && first_part;
       const size_t head0 = ((size_t)cur.b * w.kv_heads + cur.h) * a.group;
       float* part = a.part + ((size_t)blockIdx.x * 2 + (first_part ? 1 : 0)) * part_floats(a.group, D);
-      for (int x = tid; x < a.group * D / 4; x += kThreads) {
-        const int hd = x / (D / 4);
+      for (int x = tid; x < a.group * D / 2; x += kThreads) {
+        const int hd = x / (D / 2), y = x % (D / 2);
+        float2* here = reinterpret_cast<float2*>(obuf + hd * (D + kPad)) + y;
         float sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float2 o = make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) sum += wl[i * kHeads + hd];
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
-          const float4 v = *reinterpret_cast<const float4*>(obuf + i * a.group * D + 4 * x);
-          o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+          const float2 v = here[i * a.group * (D + kPad) / 2];
+          o.x += v.x; o.y += v.y;
         }
         if (a.share > 1) {                         // for the cluster: in place of the first warps' outputs
-          *reinterpret_cast<float4*>(obuf + 4 * x) = o;
-          if (x % (D / 4) == 0) ws[hd] = sum;
+          *here = o;
+          if (y == 0) ws[hd] = sum;
         } else if (whole) {
           if (!cur.bad) {
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            store4(static_cast<T*>(a.out) + head0 * D + 4 * x, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-            if (a.lse && x % (D / 4) == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (wt[hd] + log2f(sum)) * 0.69314718055994531f;
+            store2(static_cast<T*>(a.out) + (head0 + hd) * D + dim_of<kVE>(y), o.x * inv, o.y * inv);
+            if (a.lse && y == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (wt[hd] + log2f(sum)) * 0.69314718055994531f;
           }
         } else {
-          *reinterpret_cast<float4*>(part + 4 * x) = o;
-          if (x % (D / 4) == 0) { part[a.group * D + hd] = wt[hd]; part[a.group * D + kHeads + hd] = sum; }
+          reinterpret_cast<float2*>(part)[x] = o;
+          if (y == 0) { part[a.group * D + hd] = wt[hd]; part[a.group * D + kHeads + hd] = sum; }
         }
       }
       if (u + 1 == n_units && tid == 0 && !a.share) {
@@ -772,23 +781,23 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
   }
   cluster.sync();
   const size_t head0 = ((size_t)cur.b * w.kv_heads + cur.h) * a.group;
-  for (int x = rank * kThreads + tid; x < a.group * D / 4; x += a.share * kThreads) {
-    const int hd = x / (D / 4);
+  for (int x = rank * kThreads + tid; x < a.group * D / 2; x += a.share * kThreads) {
+    const int hd = x / (D / 2), y = x % (D / 2);
     float most = -INFINITY, sum = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float2 o = make_float2(0.f, 0.f);
     for (int r = 0; r < a.share; ++r) most = fmaxf(most, cluster.map_shared_rank(wt, r)[hd]);
     for (int r = 0; r < a.share; ++r) {
       const float mr = cluster.map_shared_rank(wt, r)[hd];
       if (mr == -INFINITY) continue;             // nothing there
       const float f = exp2f(mr - most);
-      const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(obuf, r) + 4 * x);
+      const float2 v = reinterpret_cast<const float2*>(cluster.map_shared_rank(obuf, r) + hd * (D + kPad))[y];
       sum += cluster.map_shared_rank(ws, r)[hd] * f;
-      o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+      o.x += v.x * f; o.y += v.y * f;
     }
     if (!cur.bad) {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      store4(static_cast<T*>(a.out) + head0 * D + 4 * x, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-      if (a.lse && x % (D / 4) == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (most + log2f(sum)) * 0.69314718055994531f;
+      store2(static_cast<T*>(a.out) + (head0 + hd) * D + dim_of<kVE>(y), o.x * inv, o.y * inv);
+      if (a.lse && y == 0) a.lse[head0 + hd] = sum == 0.f ? -INFINITY : (most + log2f(sum)) * 0.69314718055994531f;
     }
   }
   cluster.sync();                                // the others' shared memory is read until here
@@ -800,7 +809,7 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
 // carried maximum and sum from part to part waited for memory once per part (16 parts: 19 us instead of 3).
 constexpr int kJoinThreads = 256;
 
-template <typename T, int D>
+template <typename T, int D, int kVE>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeArgs a) {
   extern __shared__ float weight[];              // [heads][parts]
   __shared__ float4 slice[kJoinThreads];
@@ -852,8 +861,10 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
     o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
   }
   const float sum = total[x / (D / 4)], inv = sum == 0.f ? 0.f : 1.f / sum;
-  T* out = static_cast<T*>(a.out) + head0 * D + x * 4;
-  store4(out, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  const int hd = x / (D / 4), y = 2 * (x % (D / 4));     // two pairs of the parts' order
+  T* out = static_cast<T*>(a.out) + (head0 + hd) * D;
+  store2(out + dim_of<kVE>(y), o.x * inv, o.y * inv);
+  store2(out + dim_of<kVE>(y + 1), o.z * inv, o.w * inv);
 }
 
 template <typename T, typename C, int D>
@@ -889,7 +900,7 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
     return e;
   c->launches += 1;
   if (units <= 1 || a.share) return cudaSuccess;   // nothing is split, or joined already
-  cudaError_t e = buzz_launch_chained(paged_join_kernel<T, D>, dim3(n), (unsigned)kJoinThreads, sizeof(float) * c->group * n, stream, a);
+  cudaError_t e = buzz_launch_chained(paged_join_kernel<T, D, L::kVE>, dim3(n), (unsigned)kJoinThreads, sizeof(float) * c->group * n, stream, a);
   if (e == cudaSuccess) c->launches += 1;
   return e;
 }
