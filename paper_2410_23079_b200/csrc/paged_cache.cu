@@ -5,8 +5,9 @@
 // butterfly and the scale, is then shared by more rows), and the next rows are under way while one is worked on. 8-bit caches take
 // the row's largest magnitude by a butterfly over its lanes, on the bit patterns (as unsigned numbers a NaN
 // is above every infinity, so it is not lost). A code is the rounding of an fp32 quotient, decided at the
-// border between two codes; the quotient is estimated by a product with the scale's reciprocal (off by
-// 2^-22 of itself at most) and divided out only where a border lies that near, so that the codes are those
+// border between two codes. Rounding never goes backwards, so where a product a little below the quotient
+// and one a little above it have one code, that is the quotient's; only where they differ (mostly ties) is
+// the quotient formed. The codes are those
 // of the division (which for every element cost more than the traffic: 220 us instead of 140 for 16 prompts
 // of 4096..8192 tokens; dividing out single elements of a run instead of its eight is no faster). Because the whole page belongs to the warp, its bounds need no atomics: the
 // smallest and largest value per dimension are kept in registers over the rows and joined with the stored
@@ -95,35 +96,32 @@ __device__ __forceinline__ uint32_t row_top(const Raw<T> (&r)[2]) {
   }
 }
 
-// Eight codes of the quotients y; `near`: one of them may be on the other side of a border.
+// Eight codes of the values y times `by`, rounded to nearest, ties to even (int8: by adding 1.5 * 2^23, which
+// leaves the integer in the low bits; the codes' words are then compared with more bits than they have).
 template <typename C>
-__device__ __forceinline__ uint2 encode(const float (&y)[8], bool& near) {
-  uint32_t w[2];
+struct Codes { uint32_t n[C::kTop == 448.f ? 2 : 8]; };
+template <typename C>
+__device__ __forceinline__ Codes<C> round_codes(const float (&y)[8], float by) {
+  Codes<C> c;
+  if constexpr (C::kTop == 448.f) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if constexpr (C::kTop == 448.f) {
-      const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i], y[4 * i + 1]), __NV_SATFINITE, __NV_E4M3);
-      const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i + 2], y[4 * i + 3]), __NV_SATFINITE, __NV_E4M3);
-      w[i] = a | (b << 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        // four significant bits from 2^-6 on: borders are half steps, 2^-22 is at most four units of fp32; what is
-        // smaller and not zero is rare and divided out
-        const uint32_t u = __float_as_uint(y[4 * i + e]) & 0x7fffffffu;
-        near |= (u & 0xfffffu) - 0x7fff8u <= 0x10u || u - 1u < 0x3c7fffffu;
-      }
-    } else {
-      uint32_t n[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float t = __fadd_rn(y[4 * i + e], 12582912.f);             // 1.5 * 2^23: the integer is in the low bits
-        n[e] = __float_as_uint(t);
-        near |= fabsf(y[4 * i + e] - __fsub_rn(t, 12582912.f)) > 0.4999f;    // 2^-22 of 127 is below 2^-14
-      }
-      w[i] = __byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410);
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i] * by, y[4 * i + 1] * by), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i + 2] * by, y[4 * i + 3] * by), __NV_SATFINITE, __NV_E4M3);
+      c.n[i] = a | (b << 16);
     }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c.n[e] = __float_as_uint(__fmaf_rn(y[e], by, 12582912.f));
   }
-  return make_uint2(w[0], w[1]);
+  return c;
+}
+template <typename C>
+__device__ __forceinline__ uint2 pack_codes(const Codes<C>& c) {
+  if constexpr (C::kTop == 448.f) return make_uint2(c.n[0], c.n[1]);
+  else
+    return make_uint2(__byte_perm(__byte_perm(c.n[0], c.n[1], 0x0040), __byte_perm(c.n[2], c.n[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(c.n[4], c.n[5], 0x0040), __byte_perm(c.n[6], c.n[7], 0x0040), 0x5410));
 }
 
 // Stores a lane's elements of one row; `kLanes` lanes hold the row, two runs of eight each.
@@ -134,20 +132,25 @@ __device__ __forceinline__ void put_row(char* cache, float* scales, size_t row, 
     constexpr float kTiny = 7.888609052210118e-31f;          // 2^-100: a row of zeros has codes of zero
     if (scale < kTiny) scale = kTiny;                         // false for NaN, which stays
     if (!on) return;
-    const float inv = __frcp_rn(scale);
+    // The reciprocal is off by 2^-23 of itself, a product and the quotient that defines the code by 2^-24 each: the
+    // quotient lies between the products with factors 2^-21 below and above the reciprocal.
+    const float inv = 1.f / scale, below = inv * (1.f - 4.76837158e-7f), above = inv * (1.f + 4.76837158e-7f);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      float x[8], y[8];
-      bool near = false, never = false;
+      float x[8];
       unpack(raw[c], x);
+      Codes<C> codes = round_codes<C>(x, below);
+      const Codes<C> other = round_codes<C>(x, above);
+      uint32_t differ = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[e] * inv;
-      uint2 w = encode<C>(y, near);
-      if (near) {
+      for (int i = 0; i < (int)(sizeof(codes.n) / 4); ++i) differ |= codes.n[i] ^ other.n[i];
+      if (differ) {
+        float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = __fdiv_rn(x[e], scale);
-        w = encode<C>(y, never);
+        codes = round_codes<C>(y, 1.f);
       }
+      uint2 w = pack_codes<C>(codes);
       if (!(scale <= 3.402823466e38f)) w = make_uint2(0, 0);   // infinity or NaN: times zero it reads back as NaN
       reinterpret_cast<uint2*>(cache + row * (kLanes * 16))[c * kLanes + lane] = w;
     }
@@ -193,8 +196,8 @@ __device__ __forceinline__ void write_row(T* dst, const Kept<C>& r) {
   }
 }
 
-template <typename T, typename C, int D>
-__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 2 ? 6 : 4)
+template <typename T, typename C, int D, bool kBounds>
+__global__ void __launch_bounds__(kWarps * 32, kBounds ? (sizeof(T) == 2 ? 6 : 4) : (sizeof(T) == 2 ? 8 : 5))
 append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ v, const int32_t* cu, int total_tokens, int max_new,
               const int32_t* lens, const int32_t* table, int table_stride, int touched) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes;
@@ -224,7 +227,7 @@ append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ 
     const bool on = r < s.slot1;
     const Raw<T> kr[2] = {kn[0], kn[1]}, vr[2] = {vn[0], vn[1]};
     if (r + kRows < s.slot1) fetch(ahead);
-    if (w.bounds != nullptr && on) {
+    if (kBounds && on) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         float x[8];
@@ -236,7 +239,7 @@ append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ 
     put_row<T, C, kLanes>(w.k, w.k_scale, base + r, lane, kr, on);
     put_row<T, C, kLanes>(w.v, w.v_scale, base + r, lane, vr, on);
   }
-  if (w.bounds == nullptr) return;
+  if constexpr (!kBounds) return;
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     T* bnd = reinterpret_cast<T*>(w.bounds) + ((size_t)s.page * w.kv_heads + h) * 2 * D + c * (D / 2) + lane * 8;
@@ -310,7 +313,7 @@ cudaError_t launch(buzz_paged* c, int layer, const Call& a, cudaStream_t s) {
   const dim3 grid((unsigned)((items + kWarps - 1) / kWarps), a.batch);
   const int most = a.max_new == 1 ? 1 : touched;
   if (a.write)
-    return buzz_launch_chained(append_kernel<T, C, D>, grid, kWarps * 32, 0, s, c->view(layer), (const T*)a.k, (const T*)a.v, a.cu,
+    return buzz_launch_chained(c->buf.bounds ? append_kernel<T, C, D, true> : append_kernel<T, C, D, false>, grid, kWarps * 32, 0, s, c->view(layer), (const T*)a.k, (const T*)a.v, a.cu,
                                a.total_tokens, a.max_new, a.lens, a.table, a.table_stride, most);
   return buzz_launch_chained(read_kernel<T, C, D>, grid, kWarps * 32, 0, s, c->view(layer), (T*)a.k, (T*)a.v, a.cu, a.total_tokens,
                              a.max_new, a.lens, a.table, a.table_stride, most);

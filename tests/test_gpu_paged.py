@@ -210,6 +210,37 @@ def test_rows_with_infinities_and_nan(cuda_device, dtype, kind):
     assert torch.equal(pool.bounds[0, table[0, 0]].double().cpu(), ref.page_bounds(k, 16)[0])
 
 
+@pytest.mark.parametrize("kind,top", [(E4M3, 448.0), (I8, 127.0)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("factor", [1.0, 2.0 ** -90, 3.0, 1.7e30, 0.1])
+def test_codes_at_their_borders(cuda_device, kind, top, dtype, factor):
+    """Values on the borders between codes and one, two and three units beside them, at scales that are and are not powers of two."""
+    if kind == I8:
+        mids = torch.arange(127).double() + 0.5
+    else:
+        grid = torch.cat([torch.arange(0, 9).double() * 2.0 ** -9] + [torch.arange(8, 16).double() * 2.0 ** e for e in range(-9, 6)]).unique()
+        grid = grid[grid <= 448]
+        mids = (grid[1:] + grid[:-1]) / 2
+    rows = []
+    for shift in range(-3, 4):
+        x = (mids * factor).to(dtype)
+        bits = x.view(torch.int16 if dtype == BF16 else torch.int32)
+        rows.append((bits + shift).view(dtype) * torch.where(torch.arange(len(mids)) % 2 == 0, 1.0, -1.0).to(dtype))
+    x = torch.cat(rows)
+    n = -(-x.numel() // 63)
+    k = torch.zeros(n, 1, 64, dtype=dtype)
+    k.view(n, 64)[:, :63] = torch.cat([x, torch.zeros(63 * n - x.numel(), dtype=dtype)]).view(n, 63)
+    k[:, 0, 63] = top * factor
+    pool, table, _ = make(dtype, kind, [n], 16, 1, 1, 64, gen(1), bounds=False)
+    pool.append(0, k.to(DEV), k.to(DEV), dev_lens([n]), table.to(DEV), cu_of([n]).to(DEV))
+    assert pool.status() == 0
+    codes, scale = ref.quantise(k, kind)
+    at = torch.arange(n)
+    got = pool.k[0].view(torch.int8).cpu().view(pool.pages, 16, 64)[table[0, at // 16].long(), at % 16].view(kind).double()
+    assert torch.equal(got, codes[:, 0])
+    assert torch.equal(pool.k_scale[0].cpu().view(pool.pages, 16)[table[0, at // 16].long(), at % 16].double(), scale[:, 0])
+
+
 # ---- attention -----------------------------------------------------------------------------------
 
 def attend_case(dtype, kind, lens, page, Hq, H, d, seed, logn=False, max_len=None):
@@ -483,6 +514,21 @@ def test_a_page_listed_twice_counts_twice(cuda_device):
     rows = list(range(48, 60)) + list(range(16, 32)) * 2
     o, _, ob, _ = ref.attention(q[0], kept(ks[0][rows], I8).transpose(0, 1), kept(vs[0][rows], I8).transpose(0, 1), BF16)
     within(out[0], o, ob)
+
+
+@pytest.mark.parametrize("page", [16, 32, 128])
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+def test_selection_in_any_order(cuda_device, page, kind):
+    """The partly filled last page first and in between: its empty slots take no part wherever it stands."""
+    n = 5 * page + 3
+    pool, table, ks, vs, q, out = attend_case(BF16, kind, [n], page, 4, 1, 128, 69)
+    for order in ([5, 0, 3], [2, 5, 1], [4, 0, 5], [5, 4, 3, 2, 1, 0]):
+        sel = torch.tensor([[order]], dtype=torch.int32, device=DEV)
+        pool.decode(1, q.to(DEV), dev_lens([n]), table.to(DEV), n, out, selected=sel)
+        assert pool.status() == 0
+        rows = [i for p in order for i in range(p * page, min(n, (p + 1) * page))]
+        o, _, ob, _ = ref.attention(q[0], kept(ks[0][rows], kind).transpose(0, 1), kept(vs[0][rows], kind).transpose(0, 1), BF16)
+        within(out[0], o, ob, order)
 
 
 def test_rows_behind_the_last_sequence(cuda_device):
