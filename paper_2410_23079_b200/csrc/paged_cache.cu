@@ -7,11 +7,10 @@
 // is above every infinity, so it is not lost). A code is the rounding of an fp32 quotient, decided at the
 // border between two codes. Rounding never goes backwards, so where a product a little below the quotient
 // and one a little above it have one code, that is the quotient's; only where they differ (mostly ties) is
-// the quotient formed. The codes are those
-// of the division (which for every element cost more than the traffic: 220 us instead of 140 for 16 prompts
-// of 4096..8192 tokens; dividing out single elements of a run instead of its eight is no faster). Because the whole page belongs to the warp, its bounds need no atomics: the
-// smallest and largest value per dimension are kept in registers over the rows and joined with the stored
-// ones only if the page has older rows.
+// the quotient formed; for every element that cost more than the traffic (16 prompts of 4096..8192 tokens:
+// 220 us, now 114). Because the whole page belongs to the warp, its bounds need no atomics: the smallest and
+// largest value per dimension are kept in registers over the rows and joined with the stored ones only if the
+// page has older rows.
 // read: the same walk, the other way, four rounds of rows at a time. Both are bound by the bytes they move.
 #include "paged_internal.cuh"
 

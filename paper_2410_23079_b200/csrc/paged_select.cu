@@ -42,7 +42,11 @@ struct ScorePlan {
   static constexpr int kChunks = 2 * D / kE;                       // 16-byte chunks of a page's bounds
   static constexpr int kLanes = kChunks < 32 ? kChunks : 32;       // lanes of a page
   static constexpr int kCL = kChunks / kLanes;                     // chunks per lane
-  static constexpr int kBatches = kLanes / kBatch;                 // a lane looks up one page of its group: 32 pages a warp
+  // A lane group takes two batches: with one, the queries' sums cost as much as the pages; with four, too few warps
+  // have loads under way (131072 tokens: 17.6, 16.2 and 20.3 us for one, two and four).
+  static constexpr int kBatches = 2;
+  static constexpr int kOfGroup = kBatches * kBatch;               // pages of a lane group, looked up by a lane each
+  static constexpr int kOfWarp = 32 / kLanes * kOfGroup;
 };
 
 template <typename T>
@@ -78,14 +82,15 @@ __device__ __forceinline__ int look_up(const PagedView& w, const SelectArgs& a, 
   return -1;
 }
 
-// Keys of the 32 pages from lp0 on (those below `end`), by one warp; `mine` is the physical page of lane i's page.
+// Keys of the kOfWarp pages from lp0 on (those below `end`), by one warp; `mine` is the physical page of the lane's page,
+// number wl % kLanes of the lane group's.
 // `put(i, key)` takes the key of logical page i.
 template <typename T, int D, typename Put>
 __device__ __forceinline__ void score_pages(const PagedView& w, int h, int lp0, int end, int mine, const double* qsum, Put&& put) {
   using L = ScorePlan<T, D>;
   constexpr int kE = L::kE, kLanes = L::kLanes, kCL = L::kCL;
   const int wl = threadIdx.x & 31, lane = wl % kLanes, sub = wl / kLanes;
-  const int p0 = lp0 + sub * kLanes;                        // the lane group's pages
+  const int p0 = lp0 + sub * L::kOfGroup;                   // the lane group's pages
   uint4 raw[kBatch][kCL];
   auto fetch = [&](int batch) {
 #pragma unroll
@@ -138,6 +143,14 @@ __device__ __forceinline__ void score_pages(const PagedView& w, int h, int lp0, 
   }
 }
 
+// The physical page that score_pages wants of this lane.
+template <typename T, int D>
+__device__ __forceinline__ int look_up_mine(const PagedView& w, const SelectArgs& a, int b, int lp0, int end) {
+  using L = ScorePlan<T, D>;
+  const int wl = threadIdx.x & 31, i = wl % L::kLanes, lp = lp0 + wl / L::kLanes * L::kOfGroup + i;
+  return look_up(w, a, b, lp, i < L::kOfGroup && lp < end);
+}
+
 constexpr int kScoreWarps = 4;
 
 template <typename T, int D>
@@ -148,11 +161,12 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView
   if (len < 0 || len > a.max_len) return;                   // the pick records it
   const int count = (len + (1 << w.page_log2) - 1) >> w.page_log2;
   if (count <= a.sink + a.recent + a.top) return;
-  const int end = count - a.recent, block0 = a.sink + blockIdx.x * (kScoreWarps * 32);
+  constexpr int kOfWarp = ScorePlan<T, D>::kOfWarp;
+  const int end = count - a.recent, block0 = a.sink + blockIdx.x * (kScoreWarps * kOfWarp);
   if (block0 >= end) return;
   __shared__ double qsum[2 * D];
-  const int lp0 = block0 + (threadIdx.x & ~31), lp = lp0 + (threadIdx.x & 31);
-  const int mine = look_up(w, a, b, lp, lp < end);
+  const int lp0 = block0 + threadIdx.x / 32 * kOfWarp;
+  const int mine = look_up_mine<T, D>(w, a, b, lp0, end);
   sum_queries<T, D, kScoreWarps * 32>(a, w.kv_heads, b, h, qsum);
   __syncthreads();
   if (lp0 >= end) return;
@@ -375,13 +389,13 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const PagedView 
   const int n = pick_ends<kSelectThreads>(w, a, b, h, out);
   if (n == 0) return;
   const int end = a.sink + n;
-  int lp0 = a.sink + (threadIdx.x & ~31);
-  int mine = look_up(w, a, b, lp0 + (threadIdx.x & 31), lp0 + (int)(threadIdx.x & 31) < end);
+  constexpr int kSweep = kSelectThreads / 32 * ScorePlan<T, D>::kOfWarp;
+  int lp0 = a.sink + threadIdx.x / 32 * ScorePlan<T, D>::kOfWarp;
+  int mine = look_up_mine<T, D>(w, a, b, lp0, end);
   sum_queries<T, D, kSelectThreads>(a, w.kv_heads, b, h, qsum);
   __syncthreads();
-  for (; lp0 < end; lp0 += kSelectThreads) {
-    const int next = lp0 + kSelectThreads + (threadIdx.x & 31);
-    const int then = look_up(w, a, b, next, next < end);              // under way while these pages are scored
+  for (; lp0 < end; lp0 += kSweep) {
+    const int then = look_up_mine<T, D>(w, a, b, lp0 + kSweep, end);  // under way while these pages are scored
     score_pages<T, D>(w, h, lp0, end, mine, qsum, [&](int i, unsigned long long key) { select_keys[i - a.sink] = key; });
     mine = then;
   }
@@ -403,7 +417,8 @@ cudaError_t launch(buzz_paged* c, int layer, const SelectArgs& a, cudaStream_t s
     return e;
   }
   if (scored) {
-    const dim3 grid((middle + kScoreWarps * 32 - 1) / (kScoreWarps * 32), c->sh.kv_heads, a.batch);
+    constexpr int kOfBlock = kScoreWarps * ScorePlan<T, D>::kOfWarp;
+    const dim3 grid((middle + kOfBlock - 1) / kOfBlock, c->sh.kv_heads, a.batch);
     if (cudaError_t e = buzz_launch_chained(score_kernel<T, D>, grid, kScoreWarps * 32u, 0, s, c->view(layer), a); e != cudaSuccess) return e;
     c->launches += 1;
   }
