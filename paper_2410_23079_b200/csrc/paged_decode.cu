@@ -445,7 +445,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
 
   const int g = lane / 4, t = lane & 3;
   float oc[kOut][4], m[2], l[2];
-  float q_unit[2] = {1.f, 1.f}, v_ref = 0.f, v_unit = 0.f;   // 8-bit caches: 2^-e of a head's query, largest value scale, 2^14 over it
+  float unit[2];                                 // of a head's logits: scale, log2 e, and 2^-e of the query where it is scaled
+  float v_ref = 0.f, v_unit = 0.f;               // 8-bit caches: largest value scale, kUnit over it
   uint32_t qf[L::kQ][kKL * kMK][2];
   float s_off[2] = {0.f, 0.f};
   bool first_part = cur.unit == 0;               // the present (sequence, KV head) was begun by this block
@@ -473,22 +474,24 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
       for (int i = 0; i < kKL * kMK; ++i)
 #pragma unroll
         for (int x = 0; x < 4; ++x) big = fmaxf(big, fabsf(qv[i][x]));
-      float unit = 1.f;
+      float scale = a.scale_log2, up = 1.f;
+      if (a.logn) scale *= __logf((float)max(cur.len, 1)) * (1.0f / 6.2383246250395077f);    // log_512(tokens)
+      unit[0] = unit[1] = scale;
       if constexpr (kHalf) {
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
         const int e = max((int)(__float_as_uint(big) >> 23), 15);           // 2^(e - 127) <= big
-        unit = __uint_as_float((uint32_t)(268 - e) << 23);                   // 2^(14 - (e - 127))
+        up = __uint_as_float((uint32_t)(268 - e) << 23);                     // 2^(14 - (e - 127))
         const float back = __uint_as_float((uint32_t)(e - 14) << 23);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) q_unit[x] = __shfl_sync(0xffffffffu, back, (2 * t + x) * 4);
+        for (int x = 0; x < 2; ++x) unit[x] *= __shfl_sync(0xffffffffu, back, (2 * t + x) * 4);
       }
 #pragma unroll
       for (int i = 0; i < kKL * kMK; ++i)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           uint32_t s[L::kQ];
-          split<L::kQ, kHalf>(qv[i][2 * x] * unit, qv[i][2 * x + 1] * unit, s);
+          split<L::kQ, kHalf>(qv[i][2 * x] * up, qv[i][2 * x + 1] * up, s);
 #pragma unroll
           for (int c = 0; c < L::kQ; ++c) qf[c][i][x] = s[c];
         }
@@ -511,7 +514,8 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
     if (rows > 0) {
       const unsigned char* kt = smem + (size_t)at * 2 * L::kTileBytes;
       unsigned char* vt = smem + (size_t)at * 2 * L::kTileBytes + L::kTileBytes;
-      if (rows != (kSub == 2 ? 0x1010u : 0x10u)) {                       // what a page holds behind the sequence may be anything
+      const bool part_filled = rows != (kSub == 2 ? 0x1010u : 0x10u);
+      if (part_filled) {                       // what a page holds behind the sequence may be anything
         for (int r = 0; r < kTok; ++r) {
           if ((r & 15) < (int)(rows >> (8 * (r / 16)) & 255)) continue;
 #pragma unroll
@@ -551,22 +555,24 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
         for (int e = 0; e < 4; ++e) s[b][e] = s2[0][e] + s2[1][e];
       }
       // s[b][0], s[b][1]: key g of part b, heads 2t, 2t+1; s[b][2], s[b][3]: key g + 8
-      float scale = a.scale_log2, grow = 1.f, ks[kSub][2], vs[kSub][2];
-      bool live[kSub][2];
-      if (a.logn) scale *= __logf((float)cur.len) * (1.0f / 6.2383246250395077f);
-      float big = 0.f;
+      float grow = 1.f, ks[kSub][2], vs[kSub][2], big = 0.f;
 #pragma unroll
       for (int b = 0; b < kSub; ++b)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          live[b][y] = g + 8 * y < (int)(rows >> (8 * b) & 255);
           ks[b][y] = vs[b][y] = 1.f;
           if constexpr (C::kScaled) {
             const float* sc = scales + (size_t)at * 2 * kTok + b * 16 + g + 8 * y;
             ks[b][y] = sc[0];
-            vs[b][y] = live[b][y] ? sc[kTok] : 0.f;
-            big = fmaxf(big, vs[b][y]);
+            vs[b][y] = sc[kTok];
           }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) s[b][2 * y + e] *= C::kScaled ? ks[b][y] * unit[e] : unit[e];
+          if (part_filled && g + 8 * y >= (int)(rows >> (8 * b) & 255)) {      // whatever stands there
+            s[b][2 * y] = s[b][2 * y + 1] = -INFINITY;
+            vs[b][y] = 0.f;
+          }
+          if constexpr (C::kScaled) big = fmaxf(big, vs[b][y]);
         }
       // The maximum in use (and the largest value scale) is raised only when a logit exceeds it by more than
       // kSlack, or a scale twofold: probabilities are then 2^kSlack at most, and a tile needs no exchange
@@ -574,15 +580,9 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
       bool raise = big > 2.f * v_ref;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float unit = scale * q_unit[e], limit = m[e] + kSlack;
+        const float limit = m[e] + kSlack;
 #pragma unroll
-        for (int b = 0; b < kSub; ++b)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float& x = s[b][2 * y + e];
-            x = live[b][y] ? x * (C::kScaled ? ks[b][y] * unit : unit) : -INFINITY;
-            raise |= x > limit;
-          }
+        for (int b = 0; b < kSub; ++b) raise |= s[b][e] > limit || s[b][2 + e] > limit;
       }
       if (__any_sync(0xffffffffu, raise)) {
         if constexpr (C::kScaled) {
