@@ -432,7 +432,7 @@ class BuzzPaged:
                 _need(name in given, f"buffers: {name} is missing")
                 _tensor(name, given[name], self.device, dt, shape)
                 setattr(self, name, given[name])
-            self._status = torch.zeros(4, dtype=torch.int32, device=self.device)
+            self._status = torch.empty(4, dtype=torch.int32, device=self.device)     # zeroed by the library
             shape = _PagedShape(self.layers, self.pages, self.page_tokens, self.q_heads, self.kv_heads, self.head_dim, _DTYPES[dtype],
                                 _CACHE_DTYPES[self.cache_dtype], BUZZ_FLAG_LOGN if logn else 0)
             buf = _PagedBuffers(*[None if t is None else t.data_ptr()

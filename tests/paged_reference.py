@@ -41,7 +41,7 @@ def norm_rope(x, w, positions, inv_freq, eps, interleaved):
     return z, size * 24 * 2.0 ** -24 + z.abs() * HALF_STEP[x.dtype]
 
 
-def attention(q, k, v, dtype, scale=None):
+def attention(q, k, v, dtype, scale=None, kind=None):
     """One sequence: q [Hq, d], k and v [Hkv, n, d] in 64 bits. Returns (out, lse, out bound, lse bound)."""
     Hq, d = q.shape
     H, n = k.shape[:2]
@@ -56,11 +56,16 @@ def attention(q, k, v, dtype, scale=None):
     # maximum; fp32 operands lose 2^-23 to their three bf16 parts, which the first term's slack of two covers
     es = (2 * d * 2.0 ** -24 * torch.einsum("hgd,hnd->hgn", q.abs(), k.abs()).amax(-1) * abs(scale) + 6 * 2.0 ** -24 * s.abs().amax(-1)).unsqueeze(-1)
     # a probability: its logit's error, exp2 (2^-22), up to n additions to the sum in chains of n/16 or fewer and rescalings;
-    # its parts for the product: 2^-16 for bf16 outputs, 2^-23 for fp32
+    # its parts for the product: 2^-16 for bf16 outputs, 2^-22 for fp32. Of an 8-bit cache (kind) and bf16 outputs it is one
+    # fp16 number: half a step, 2^-11 of it, or, below fp16's normal range, of 2^-24 in units of 2^-8 (the kernel gives a
+    # probability of 1 at the largest value scale the weight 2^8), per key and times the largest value
     ep = 2 * es + 2.0 ** -21 + (n / 16 + 40) * 2.0 ** -24
-    parts = 2.0 ** -16 if dtype == torch.bfloat16 else 2.0 ** -22
+    single = dtype == torch.bfloat16 and kind in TOP
+    parts = 2.0 ** -11 if single else 2.0 ** -16 if dtype == torch.bfloat16 else 2.0 ** -22
     weight = torch.einsum("hgn,hnd->hgd", p, v.abs())
     bound = weight * (ep + parts) + out.abs() * HALF_STEP[dtype]
+    if single:
+        bound = bound + n * 2.0 ** -33 * v.abs().amax((1, 2))[:, None, None]
     return out.view(Hq, d), lse.view(Hq), bound.view(Hq, d), (ep.squeeze(-1) + lse.abs() * 2.0 ** -22).view(Hq)
 
 

@@ -256,7 +256,7 @@ def attend_case(dtype, kind, lens, page, Hq, H, d, seed, logn=False, max_len=Non
     assert pool.status() == 0
     for b, n in enumerate(lens):
         scale = d ** -0.5 * (math.log(max(n, 1)) / math.log(512) if logn else 1.0)
-        o, e, ob, eb = ref.attention(q[b], kept(ks[b], kind).transpose(0, 1), kept(vs[b], kind).transpose(0, 1), dtype, scale)
+        o, e, ob, eb = ref.attention(q[b], kept(ks[b], kind).transpose(0, 1), kept(vs[b], kind).transpose(0, 1), dtype, scale, kind)
         within(out[b], o, ob, ("out", b, n))
         within(lse[b], e, eb, ("lse", b, n))
     return pool, table, ks, vs, q, out
@@ -340,7 +340,7 @@ def test_decode_bad_lengths_and_pages(cuda_device):
         assert pool.status() == -1
         assert torch.equal(out[:2], good[:2])
         keep = [i for i in range(70) if not 16 <= i < 32]
-        o, _, ob, _ = ref.attention(q[2], kept(ks[2][keep], E4M3).transpose(0, 1), kept(vs[2][keep], E4M3).transpose(0, 1), BF16)
+        o, _, ob, _ = ref.attention(q[2], kept(ks[2][keep], E4M3).transpose(0, 1), kept(vs[2][keep], E4M3).transpose(0, 1), BF16, kind=E4M3)
         within(out[2], o, ob)
 
 
@@ -412,7 +412,7 @@ def select_case(dtype, kind, lens, page, Hq, H, d, sink, recent, top, seed, tie=
         k, v = kept(ks[b], kind).transpose(0, 1), kept(vs[b], kind).transpose(0, 1)
         for h in range(H):
             rows = [i for p in want[h] for i in range(p * page, min(m, (p + 1) * page))]
-            o, e, ob, eb = ref.attention(q[b, h * G:(h + 1) * G], k[h:h + 1, rows], v[h:h + 1, rows], dtype)
+            o, e, ob, eb = ref.attention(q[b, h * G:(h + 1) * G], k[h:h + 1, rows], v[h:h + 1, rows], dtype, kind=kind)
             within(out[b, h * G:(h + 1) * G], o, ob, (b, h))
             within(lse[b, h * G:(h + 1) * G], e, eb, (b, h))
 
@@ -512,7 +512,7 @@ def test_a_page_listed_twice_counts_twice(cuda_device):
     pool.decode(1, q.to(DEV), dev_lens([60]), table.to(DEV), 60, out, selected=torch.tensor([[[3, 1, 1]]], dtype=torch.int32, device=DEV))
     assert pool.status() == 0
     rows = list(range(48, 60)) + list(range(16, 32)) * 2
-    o, _, ob, _ = ref.attention(q[0], kept(ks[0][rows], I8).transpose(0, 1), kept(vs[0][rows], I8).transpose(0, 1), BF16)
+    o, _, ob, _ = ref.attention(q[0], kept(ks[0][rows], I8).transpose(0, 1), kept(vs[0][rows], I8).transpose(0, 1), BF16, kind=I8)
     within(out[0], o, ob)
 
 
@@ -527,7 +527,7 @@ def test_selection_in_any_order(cuda_device, page, kind):
         pool.decode(1, q.to(DEV), dev_lens([n]), table.to(DEV), n, out, selected=sel)
         assert pool.status() == 0
         rows = [i for p in order for i in range(p * page, min(n, (p + 1) * page))]
-        o, _, ob, _ = ref.attention(q[0], kept(ks[0][rows], kind).transpose(0, 1), kept(vs[0][rows], kind).transpose(0, 1), BF16)
+        o, _, ob, _ = ref.attention(q[0], kept(ks[0][rows], kind).transpose(0, 1), kept(vs[0][rows], kind).transpose(0, 1), BF16, kind=kind)
         within(out[0], o, ob, order)
 
 
@@ -678,13 +678,13 @@ def test_prompts_then_steps_of_one_layer(cuda_device, kind, captured):
                     pages, slot = table[b, torch.arange(m) // page].long(), torch.arange(m) % page
                     rows = lambda z, s: z[0].view(torch.int8).cpu()[pages, :, slot].view(E4M3).double() * s[0].cpu()[pages, :, slot].double()[..., None]
                     kk, vv = rows(pool.k, pool.k_scale), rows(pool.v, pool.v_scale)
-                o, _, ob, _ = ref.attention(q_rot[b].cpu(), kk.transpose(0, 1), vv.transpose(0, 1), BF16)
+                o, _, ob, _ = ref.attention(q_rot[b].cpu(), kk.transpose(0, 1), vv.transpose(0, 1), BF16, kind=kind)
                 within(out[b], o, ob, (i, b))
                 want = sel[b].tolist()
                 for h in range(H):
                     at = [r for p in want[h] if p >= 0 for r in range(p * page, min(m, (p + 1) * page))]
                     G = Hq // H
-                    o, _, ob, _ = ref.attention(q_rot[b, h * G:(h + 1) * G].cpu(), kk.transpose(0, 1)[h:h + 1, at], vv.transpose(0, 1)[h:h + 1, at], BF16)
+                    o, _, ob, _ = ref.attention(q_rot[b, h * G:(h + 1) * G].cpu(), kk.transpose(0, 1)[h:h + 1, at], vv.transpose(0, 1)[h:h + 1, at], BF16, kind=kind)
                     within(sparse[b, h * G:(h + 1) * G], o, ob, (i, b, h))
     assert pool.status() == 0
 
