@@ -11,7 +11,9 @@
 // 220 us, now 114). Because the whole page belongs to the warp, its bounds need no atomics: the smallest and
 // largest value per dimension are kept in registers over the rows and joined with the stored ones only if the
 // page has older rows.
-// read: the same walk, the other way, four rounds of rows at a time. Both are bound by the bytes they move.
+// read: the same walk, the other way, four rounds of rows at a time. Both are bound by the bytes they move:
+// those prompts (607 MB each way) are written in 114 us, 0.82 of the measured copy bandwidth (97 M warp
+// instructions share the time), and read in 107 us, 0.88.
 #include "paged_internal.cuh"
 
 namespace {
