@@ -795,11 +795,11 @@ paged_decode_kernel(const PagedView w, const DecodeArgs a, const __grid_constant
     float2 o = make_float2(0.f, 0.f);
     for (int r = 0; r < a.share; ++r) most = fmaxf(most, cluster.map_shared_rank(wt, r)[hd]);
     for (int r = 0; r < a.share; ++r) {
-      const float mr = cluster.map_shared_rank(wt, r)[hd];
-      if (mr == -INFINITY) continue;             // nothing there
-      const float f = exp2f(mr - most);
+      const float mr = cluster.map_shared_rank(wt, r)[hd], sr = cluster.map_shared_rank(ws, r)[hd];
+      if (mr == -INFINITY && sr == 0.f) continue;    // nothing there (a sum of NaN without a maximum is something)
+      const float f = mr == -INFINITY ? 0.f : exp2f(mr - most);
       const float2 v = reinterpret_cast<const float2*>(cluster.map_shared_rank(obuf, r) + hd * (D + kPad))[y];
-      sum += cluster.map_shared_rank(ws, r)[hd] * f;
+      sum += sr * f;
       o.x += v.x * f; o.y += v.y * f;
     }
     if (!cur.bad) {

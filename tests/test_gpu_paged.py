@@ -322,6 +322,32 @@ def test_decode_logits_of_minus_infinity_and_extreme_scales(cuda_device):
     assert torch.equal(out.cpu(), torch.zeros(1, 1, 64, dtype=BF16)) and float(lse) == -math.inf
 
 
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("H,lens", [(1, [1100]), (2, [9000]), (8, [1100] * 20)])
+def test_decode_does_not_lose_a_nan(cuda_device, dtype, kind, H, lens):
+    """Keys that are NaN, a tile or a block's whole share of them: the output of their sequence and head is NaN, the
+    others are as without them. A cluster per head, the line, more heads than SMs."""
+    g = gen(22)
+    pool, table, _ = make(dtype, kind, lens, 16, H, H, 128, g)
+    k, v = [torch.randn(sum(lens), H, 128, generator=g).to(dtype).to(DEV) for _ in range(2)]
+    q = torch.randn(len(lens), H, 128, generator=g).to(dtype).to(DEV)
+    t = table.to(DEV)
+    pool.append(0, k, v, dev_lens(lens), t, cu_of(lens).to(DEV), max(lens))
+    good, out = torch.empty_like(q), torch.empty_like(q)
+    pool.decode(0, q, dev_lens(lens), t, max(lens), good)
+    assert bool(good.isfinite().all())
+    for lo, hi in ((0, lens[0]), (0, 160), (384, 800), (lens[0] - 1, lens[0])):
+        bad = k.clone()
+        bad[lo:hi, 0] = math.nan
+        pool.append(0, bad, v, dev_lens(lens), t, cu_of(lens).to(DEV), max(lens))
+        lse = torch.zeros(len(lens), H, device=DEV)
+        pool.decode(0, q, dev_lens(lens), t, max(lens), out, lse=lse)
+        assert bool(out[0, 0].isnan().all()) and bool(lse[0, 0].isnan()), (lo, hi)
+        out[0, 0] = good[0, 0]
+        assert torch.equal(out, good), (lo, hi)
+    assert pool.status() == 0
+
+
 def test_decode_bad_lengths_and_pages(cuda_device):
     g = gen(31)
     lens = [100, 50, 70]
