@@ -381,11 +381,11 @@ int buzz_paged_read(buzz_paged_t ctx, int layer, void* k_out, void* v_out, const
                     int batch, int total_tokens, int max_new, const int32_t* lens_dev,
                     const int32_t* table_dev, int table_stride, void* stream);
 
-/* Workspace that one buzz_paged_decode and one buzz_paged_select call of this size need. It holds
- * nothing between calls; calls that may run at the same time need one each. Where 0 bytes are needed the
- * call takes NULL. */
-int buzz_paged_workspace_bytes(buzz_paged_t ctx, int batch, int max_len, size_t* decode_bytes,
-                               size_t* select_bytes);
+/* Workspace that one buzz_paged_decode (with that `selected_stride`, 0: without a selection) and one
+ * buzz_paged_select call of this size need; either pointer may be NULL. It holds nothing between calls;
+ * calls that may run at the same time need one each. Where 0 bytes are needed the call takes NULL. */
+int buzz_paged_workspace_bytes(buzz_paged_t ctx, int batch, int max_len, int selected_stride,
+                               size_t* decode_bytes, size_t* select_bytes);
 
 /* Attention of one new token per sequence over its pages: q, out [batch][Hq][d], out = Softmax(q k^T /
  * sqrt(d)) v over the lens[b] tokens; lse fp32 [batch][Hq] (or NULL) receives the natural logarithm

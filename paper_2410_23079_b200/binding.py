@@ -124,7 +124,7 @@ def load_library(build_if_missing: bool = True):
     lib.buzz_paged_read.restype = ci
     lib.buzz_paged_read.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, vp, vp, ci, vp]
     lib.buzz_paged_workspace_bytes.restype = ci
-    lib.buzz_paged_workspace_bytes.argtypes = [vp, ci, ci, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.buzz_paged_workspace_bytes.argtypes = [vp, ci, ci, ci, ctypes.POINTER(sz), ctypes.POINTER(sz)]
     lib.buzz_paged_decode.restype = ci
     lib.buzz_paged_decode.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, vp, ci, vp, vp, vp, sz, vp]
     lib.buzz_paged_select.restype = ci
@@ -329,28 +329,43 @@ def _token_stride(name, x, device, dtype, tokens, heads, d):
     raise ValueError(f"{name}: a token's heads are not contiguous")
 
 
-class _On:
-    """Makes `device` current for a call that launches on `stream` (None: the device's current one), with what the
-    call allocates belonging to that stream, and restores what was. A given stream has to be one of that device."""
-    __slots__ = ("ptr", "guard")
+class _Here:
+    """A stream's handle as a context that changes nothing: the call's device is current, and so is its stream."""
+    __slots__ = ("ptr",)
 
-    def __init__(self, device, stream):
-        if stream is None:
-            self.ptr = torch._C._cuda_getCurrentRawStream(device.index)
-            self.guard = torch.cuda.device(device) if torch._C._cuda_getDevice() != device.index else None
-        else:
-            _need(stream.device == device, f"stream: of {stream.device}, not of {device}")
-            self.ptr = stream.cuda_stream
-            self.guard = torch.cuda.stream(stream)
+    def __init__(self, ptr):
+        self.ptr = ptr
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
         return self.ptr
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        pass
+
+
+class _There:
+    """The same with another device or stream made current for the call, so that what it allocates belongs to that
+    stream, and what was current restored."""
+
+    def __init__(self, ptr, guard):
+        self.ptr, self.guard = ptr, guard
+
+    def __enter__(self):
+        self.guard.__enter__()
+        return self.ptr
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+def _on(device, stream):
+    """Context of a call that launches on `stream` (None: the device's current one); its value is the stream's handle. A
+    given stream has to be one of that device."""
+    if stream is None:
+        ptr = torch._C._cuda_getCurrentRawStream(device.index)
+        return _Here(ptr) if torch._C._cuda_getDevice() == device.index else _There(ptr, torch.cuda.device(device))
+    _need(stream.device == device, f"stream: of {stream.device}, not of {device}")
+    return _There(stream.cuda_stream, torch.cuda.stream(stream))
 
 
 def _cuda_device(device) -> torch.device:
@@ -379,7 +394,7 @@ def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps=1e
     qw = None if q_weight is None else _tensor("q_weight", q_weight, device, dtype, (d,))
     kw = None if k_weight is None else _tensor("k_weight", k_weight, device, dtype, (d,))
     qs, ks = _token_stride("q", q, device, dtype, T, Hq, d), _token_stride("k", k, device, dtype, T, Hk, d)
-    with _On(device, stream) as s:
+    with _on(device, stream) as s:
         if q_out is None:
             q_out, qos = torch.empty_like(q, memory_format=torch.contiguous_format), Hq * d
         else:
@@ -440,7 +455,6 @@ class BuzzPaged:
             h = ctypes.c_void_p()
             _check(self._lib.buzz_paged_create(ctypes.byref(h), ctypes.byref(shape), ctypes.byref(buf)), "buzz_paged_create")
         self._h = h
-        self._decode_bytes = self._scratch_bytes(1, 0)[0]
 
     def close(self):
         if self._h is not None:
@@ -471,8 +485,10 @@ class BuzzPaged:
         else:
             cu = _tensor("cu_seqlens", cu_seqlens, self.device, torch.int32, (batch + 1,))
             max_new = k.shape[0] if max_new is None else max_new
-        with _On(self.device, stream) as s:
-            _check(call(self._h, layer, kp, vp, cu, batch, k.shape[0], max_new, lp, tp, stride, s), where)
+        with _on(self.device, stream) as s:
+            rc = call(self._h, layer, kp, vp, cu, batch, k.shape[0], max_new, lp, tp, stride, s)
+        if rc:
+            raise BuzzError(rc, where)
 
     def append(self, layer, k, v, lens, table, cu_seqlens=None, max_new=None, stream=None):
         """buzz_paged_append: k, v [tokens, Hkv, d] become the last tokens of their sequences; `lens` counts them."""
@@ -482,26 +498,31 @@ class BuzzPaged:
         """buzz_paged_read: the last tokens of every sequence, as they are kept, to k_out, v_out [tokens, Hkv, d]."""
         self._rows("buzz_paged_read", self._lib.buzz_paged_read, layer, k_out, v_out, lens, table, cu_seqlens, max_new, stream)
 
-    def _scratch_bytes(self, batch, max_len):
-        """Bytes of a decode's workspace (the same for every call) and of a select's. The workspaces themselves are made
-        per call, by the framework's allocator and for the call's stream, so that no two calls share one."""
-        decode, select = ctypes.c_size_t(), ctypes.c_size_t()
-        _check(self._lib.buzz_paged_workspace_bytes(self._h, batch, max_len, decode, select), "buzz_paged_workspace_bytes")
-        return decode.value, select.value
+    def _workspace(self, batch, max_len, selected_stride, of_select):
+        """(tensor, bytes) of a call's workspace, (None, 0) where it needs none. It is made per call, by the framework's
+        allocator and for the call's stream, so that no two calls share one."""
+        n = ctypes.c_size_t()
+        rc = self._lib.buzz_paged_workspace_bytes(self._h, batch, max_len, selected_stride, None if of_select else n, n if of_select else None)
+        if rc:
+            raise BuzzError(rc, "buzz_paged_workspace_bytes")
+        n = n.value
+        return (torch.empty(n, dtype=torch.uint8, device=self.device), n) if n else (None, 0)
 
     def decode(self, layer, q, lens, table, max_len, out, lse=None, selected=None, stream=None):
         """buzz_paged_decode: attention of one token per sequence, q and out [batch, Hq, d], lse fp32 [batch, Hq] or None;
         `selected` int32 [batch, Hkv, n] limits it to those logical pages."""
-        batch, lp, tp, stride = self._sequences(lens, table)
+        batch, lp, tp, width = self._sequences(lens, table)
         shape = (batch, self.q_heads, self.head_dim)
         qp, op = _tensor("q", q, self.device, self.dtype, shape), _tensor("out", out, self.device, self.dtype, shape)
         ep = None if lse is None else _tensor("lse", lse, self.device, torch.float32, (batch, self.q_heads))
         sp = None if selected is None else _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, None))
-        with _On(self.device, stream) as s:
-            n = self._decode_bytes
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            _check(self._lib.buzz_paged_decode(self._h, layer, qp, lp, tp, stride, batch, max_len, sp,
-                                               0 if selected is None else selected.shape[2], op, ep, ws.data_ptr(), n, s), "buzz_paged_decode")
+        stride = 0 if selected is None else selected.shape[2]
+        with _on(self.device, stream) as s:
+            ws, n = self._workspace(batch, max_len, stride, False)
+            rc = self._lib.buzz_paged_decode(self._h, layer, qp, lp, tp, width, batch, max_len, sp, stride, op, ep,
+                                             None if ws is None else ws.data_ptr(), n, s)
+        if rc:
+            raise BuzzError(rc, "buzz_paged_decode")
 
     def select(self, layer, q, lens, table, max_len, sink, recent, top, selected, stream=None):
         """buzz_paged_select: the pages for `decode`, into `selected` int32 [batch, Hkv, sink + recent + top]."""
@@ -509,15 +530,15 @@ class BuzzPaged:
         _need(self.bounds is not None, "the pool has no bounds")
         qp = _tensor("q", q, self.device, self.dtype, (batch, self.q_heads, self.head_dim))
         sp = _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, sink + recent + top))
-        with _On(self.device, stream) as s:
-            n = self._scratch_bytes(batch, max_len)[1]
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
-            _check(self._lib.buzz_paged_select(self._h, layer, qp, lp, tp, stride, batch, max_len, sink, recent, top, sp,
-                                               None if ws is None else ws.data_ptr(), n, s),
-                   "buzz_paged_select")
+        with _on(self.device, stream) as s:
+            ws, n = self._workspace(batch, max_len, 0, True)
+            rc = self._lib.buzz_paged_select(self._h, layer, qp, lp, tp, stride, batch, max_len, sink, recent, top, sp,
+                                             None if ws is None else ws.data_ptr(), n, s)
+        if rc:
+            raise BuzzError(rc, "buzz_paged_select")
 
     def status(self, stream=None) -> int:
-        with _On(self.device, stream) as s:
+        with _on(self.device, stream) as s:
             return self._lib.buzz_paged_status(self._h, s)
 
     def launch_count(self) -> int:

@@ -70,16 +70,18 @@ struct DecodeArgs {
 
 __host__ __device__ constexpr int part_floats(int group, int d) { return group * d + 2 * kHeads; }      // a multiple of four
 
+// Warps and the stages of their rings fill 200 KB. 8-bit rows cost so many instructions per byte that
+// twelve warps with two stages are faster than eight with three (161 -> 147 us on the rows above); wider
+// rows wait for memory, and fewer warps mean fewer parts to merge.
+constexpr int warps_for(int row_bytes, bool scaled) { return row_bytes >= 256 ? 4 : scaled ? 12 : 8; }
+
 template <typename T, typename C, int D>
 struct Plan {
   static constexpr bool kHalf = C::kScaled;            // fp16 operands
   static constexpr int kRow = D * C::kSize;            // bytes of a row
   static constexpr int kTok = buzz_paged_tile_tokens(kRow);
   static constexpr int kSub = kTok / 16;               // 16-row parts of a tile
-  // Warps and the stages of their rings fill 200 KB. 8-bit rows cost so many instructions per byte that
-  // twelve warps with two stages are faster than eight with three (161 -> 147 us on the rows above); wider
-  // rows wait for memory, and fewer warps mean fewer parts to merge.
-  static constexpr int kWarps = kRow >= 256 ? 4 : C::kScaled ? 12 : 8;
+  static constexpr int kWarps = warps_for(kRow, C::kScaled);
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kBox = buzz_paged_box_bytes(kRow);
   static constexpr int kBoxes = kRow / kBox;
@@ -875,16 +877,18 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const DecodeAr
   store2(out + dim_of<kVE>(y + 1), o.z * inv, o.w * inv);
 }
 
-template <typename T, typename C, int D>
-cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) {
-  using L = Plan<T, C, D>;
-  long long tokens = a.max_len;
-  if (a.selected) {
-    const long long most = (long long)a.selected_stride << c->page_log2, round = ((tokens >> c->page_log2) + 1) << c->page_log2;
+// How a call is spread: units of a (sequence, KV head) at most, and the blocks of the cluster that takes one (0: blocks
+// take stretches of the line, and there is a join).
+struct Spread { long long units; int share; };
+
+Spread spread(const buzz_paged* c, int batch, int max_len, bool selected, int selected_stride) {
+  const int row = (int)(c->sh.head_dim * c->csize), of_unit = buzz_paged_tile_tokens(row) * warps_for(row, c->buf.k_scale != nullptr);
+  long long tokens = max_len;
+  if (selected) {
+    const long long most = (long long)selected_stride << c->page_log2, round = ((tokens >> c->page_log2) + 1) << c->page_log2;
     tokens = most < round ? most : round;
   }
-  const long long units = (tokens + L::kTok * L::kWarps - 1) / (L::kTok * L::kWarps);          // of a (sequence, KV head), at most
-  const long long all = (long long)a.batch * c->sh.kv_heads * (units > 0 ? units : 1);
+  const long long units = (tokens + of_unit - 1) / of_unit;
   // Few (sequence, KV head)s and little to read: each gets a cluster of 1 to 8 blocks of its own, which join their
   // parts in shared memory. The join through global memory is a second launch (4 us on the host) and takes the
   // GPU 3 us longer, the time of two units, so the cluster is taken while a block of it reads at most two units
@@ -893,12 +897,19 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
   // 14.9, 14.8; 72 x 2048 25.2, 20.2. Eight units at most, since lengths may differ. Sixteen clusters of eight
   // do not find SMs at once (16 heads x 517 tokens: 14.0 us, with clusters of four 8.7): four from 9 heads on,
   // two from 33 on.
-  const long long heads = (long long)a.batch * c->sh.kv_heads;
+  const long long heads = (long long)batch * c->sh.kv_heads;
   int share = heads <= 8 ? 8 : heads <= 32 ? 4 : heads <= 64 ? 2 : 1;
   while (share > 1 && share / 2 >= units) share /= 2;
   const long long each = (units + share - 1) / share, even = (units * heads + c->sm_count - 1) / c->sm_count;
-  a.share = heads <= c->sm_count && each <= 8 && each <= even + 2 ? share : 0;
-  const int n = (int)(a.share ? heads * share : all < c->sm_count ? all : c->sm_count);
+  return Spread{units, heads <= c->sm_count && each <= 8 && each <= even + 2 ? share : 0};
+}
+
+template <typename T, typename C, int D>
+cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, const Spread& sp, cudaStream_t stream) {
+  using L = Plan<T, C, D>;
+  const long long heads = (long long)a.batch * c->sh.kv_heads, all = heads * (sp.units > 0 ? sp.units : 1);
+  a.share = sp.share;
+  const int n = (int)(a.share ? heads * a.share : all < c->sm_count ? all : c->sm_count);
   const size_t smem = L::smem(c->group);
   static BuzzSmemOptIn opt_in;
   if (cudaError_t e = opt_in.ensure(paged_decode_kernel<T, C, D>, smem); e != cudaSuccess) return e;
@@ -907,22 +918,26 @@ cudaError_t launch(buzz_paged* c, int layer, DecodeArgs a, cudaStream_t stream) 
       e != cudaSuccess)
     return e;
   c->launches += 1;
-  if (units <= 1 || a.share) return cudaSuccess;   // nothing is split, or joined already
+  if (sp.units <= 1 || a.share) return cudaSuccess;   // nothing is split, or joined already
   cudaError_t e = buzz_launch_chained(paged_join_kernel<T, D, L::kVE>, dim3(n), (unsigned)kJoinThreads, sizeof(float) * c->group * n, stream, a);
   if (e == cudaSuccess) c->launches += 1;
   return e;
 }
 
 template <typename T, typename C>
-cudaError_t launch_d(buzz_paged* c, int layer, const DecodeArgs& a, cudaStream_t s) {
-  return c->sh.head_dim == 128 ? launch<T, C, 128>(c, layer, a, s) : launch<T, C, 64>(c, layer, a, s);
+cudaError_t launch_d(buzz_paged* c, int layer, const DecodeArgs& a, const Spread& sp, cudaStream_t s) {
+  return c->sh.head_dim == 128 ? launch<T, C, 128>(c, layer, a, sp, s) : launch<T, C, 64>(c, layer, a, sp, s);
 }
 
 }  // namespace
 
-// bytes of a decode call's workspace: a descriptor and two parts per block
-size_t buzz_paged_decode_workspace(const buzz_paged* c) {
-  return (size_t)c->sm_count * (sizeof(int4) + 2 * sizeof(float) * part_floats(c->group, c->sh.head_dim));
+// bytes of a decode call's workspace: a descriptor and two parts per block of the line
+static size_t decode_workspace(const buzz_paged* c, const Spread& sp) {
+  return sp.share ? 0 : (size_t)c->sm_count * (sizeof(int4) + 2 * sizeof(float) * part_floats(c->group, c->sh.head_dim));
+}
+
+size_t buzz_paged_decode_workspace(const buzz_paged* c, int batch, int max_len, int selected_stride) {
+  return decode_workspace(c, spread(c, batch, max_len, selected_stride > 0, selected_stride));
 }
 
 extern "C" int buzz_paged_decode(buzz_paged_t c, int layer, const void* q, const int32_t* lens_dev, const int32_t* table_dev,
@@ -930,11 +945,13 @@ extern "C" int buzz_paged_decode(buzz_paged_t c, int layer, const void* q, const
                                  float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (!c || layer < 0 || layer >= c->sh.layers || batch < 1 || batch > 65535 || table_stride < 1) return BUZZ_ERR_INVALID;
   if (max_len < 0 || max_len > (int64_t)table_stride * c->sh.page_tokens) return BUZZ_ERR_INVALID;
-  if (!q || !lens_dev || !table_dev || !out || !workspace || (selected && selected_stride < 1)) return BUZZ_ERR_INVALID;
+  if (!q || !lens_dev || !table_dev || !out || (selected && selected_stride < 1)) return BUZZ_ERR_INVALID;
+  const Spread sp = spread(c, batch, max_len, selected != nullptr, selected_stride);
+  const size_t need = decode_workspace(c, sp);
   const uintptr_t wide = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace);
   const uintptr_t words = reinterpret_cast<uintptr_t>(lens_dev) | reinterpret_cast<uintptr_t>(table_dev) |
                           reinterpret_cast<uintptr_t>(selected) | reinterpret_cast<uintptr_t>(lse);
-  if ((wide & 15u) || (words & 3u) || workspace_bytes < buzz_paged_decode_workspace(c)) return BUZZ_ERR_INVALID;
+  if ((wide & 15u) || (words & 3u) || workspace_bytes < need || (need > 0 && !workspace)) return BUZZ_ERR_INVALID;
   DecodeArgs a;
   a.q = q; a.out = out; a.lse = lse;
   a.lens = lens_dev; a.table = table_dev; a.selected = selected;
@@ -949,10 +966,10 @@ extern "C" int buzz_paged_decode(buzz_paged_t c, int layer, const void* q, const
   cudaError_t e = cudaErrorInvalidValue;
   const bool f32 = c->sh.dtype == BUZZ_F32;
   switch (c->sh.cache_dtype) {
-    case BUZZ_F32: e = launch_d<float, CacheF32>(c, layer, a, s); break;
-    case BUZZ_BF16: e = launch_d<__nv_bfloat16, CacheBF16>(c, layer, a, s); break;
-    case BUZZ_E4M3: e = f32 ? launch_d<float, CacheE4M3>(c, layer, a, s) : launch_d<__nv_bfloat16, CacheE4M3>(c, layer, a, s); break;
-    case BUZZ_I8: e = f32 ? launch_d<float, CacheI8>(c, layer, a, s) : launch_d<__nv_bfloat16, CacheI8>(c, layer, a, s); break;
+    case BUZZ_F32: e = launch_d<float, CacheF32>(c, layer, a, sp, s); break;
+    case BUZZ_BF16: e = launch_d<__nv_bfloat16, CacheBF16>(c, layer, a, sp, s); break;
+    case BUZZ_E4M3: e = f32 ? launch_d<float, CacheE4M3>(c, layer, a, sp, s) : launch_d<__nv_bfloat16, CacheE4M3>(c, layer, a, sp, s); break;
+    case BUZZ_I8: e = f32 ? launch_d<float, CacheI8>(c, layer, a, sp, s) : launch_d<__nv_bfloat16, CacheI8>(c, layer, a, sp, s); break;
   }
   return e == cudaSuccess ? BUZZ_OK : BUZZ_ERR_CUDA;
 }

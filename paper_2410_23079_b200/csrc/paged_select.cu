@@ -436,7 +436,7 @@ cudaError_t launch(buzz_paged* c, int layer, const SelectArgs& a, cudaStream_t s
 
 }  // namespace
 
-size_t buzz_paged_decode_workspace(const buzz_paged* c);
+size_t buzz_paged_decode_workspace(const buzz_paged* c, int batch, int max_len, int selected_stride);
 
 static size_t select_workspace(const buzz_paged* c, int batch, int max_len) {
   const size_t pages = ((size_t)max_len + c->sh.page_tokens - 1) / c->sh.page_tokens;
@@ -444,10 +444,11 @@ static size_t select_workspace(const buzz_paged* c, int batch, int max_len) {
   return (size_t)batch * c->sh.kv_heads * pages * sizeof(unsigned long long);
 }
 
-extern "C" int buzz_paged_workspace_bytes(buzz_paged_t c, int batch, int max_len, size_t* decode_bytes, size_t* select_bytes) {
-  if (!c || !decode_bytes || !select_bytes || batch < 1 || batch > 65535 || max_len < 0) return BUZZ_ERR_INVALID;
-  *decode_bytes = buzz_paged_decode_workspace(c);
-  *select_bytes = select_workspace(c, batch, max_len);
+extern "C" int buzz_paged_workspace_bytes(buzz_paged_t c, int batch, int max_len, int selected_stride, size_t* decode_bytes,
+                                          size_t* select_bytes) {
+  if (!c || batch < 1 || batch > 65535 || max_len < 0 || selected_stride < 0) return BUZZ_ERR_INVALID;
+  if (decode_bytes) *decode_bytes = buzz_paged_decode_workspace(c, batch, max_len, selected_stride);
+  if (select_bytes) *select_bytes = select_workspace(c, batch, max_len);
   return BUZZ_OK;
 }
 

@@ -620,9 +620,13 @@ def test_refusals(cuda_device):
         assert e.value.code == -1
     n = ctypes.c_size_t()
     lib, h = pool._lib, pool._h
-    assert lib.buzz_paged_workspace_bytes(h, 0, 1, ctypes.byref(n), ctypes.byref(n)) == -1
-    assert lib.buzz_paged_decode(h, 0, q.data_ptr(), lens.data_ptr(), t.data_ptr(), t.shape[1], 2, 40, None, 0, out.data_ptr(), None,
-                                 x.data_ptr(), 8, None) == -1                      # a workspace that is too small
+    assert lib.buzz_paged_workspace_bytes(h, 0, 1, 0, ctypes.byref(n), ctypes.byref(n)) == -1
+    assert lib.buzz_paged_workspace_bytes(h, 1, 1, -1, ctypes.byref(n), ctypes.byref(n)) == -1
+    many = torch.zeros(2, 60000, dtype=torch.int32, device=DEV)
+    assert lib.buzz_paged_workspace_bytes(h, 2, 960000, 0, ctypes.byref(n), None) == 0 and n.value > 0
+    for ws, size in ((None, n.value), (x.data_ptr(), n.value - 1), (x.data_ptr() + 8, n.value)):     # none, too small, misaligned
+        assert lib.buzz_paged_decode(h, 0, q.data_ptr(), lens.data_ptr(), many.data_ptr(), 60000, 2, 960000, None, 0, out.data_ptr(), None,
+                                     ws, size, None) == -1
     wide = torch.zeros(2, 600, dtype=torch.int32, device=DEV)
     for ws in (None, x.data_ptr()):                           # no workspace, and one that is too small
         assert lib.buzz_paged_select(h, 0, q.data_ptr(), lens.data_ptr(), wide.data_ptr(), 600, 2, 9600, 1, 1, 1, sel.data_ptr(), ws, 8, None) == -1

@@ -55,7 +55,7 @@ def test_paged_buffers(over):
 
 def test_calls_without_an_object():
     n = ctypes.c_size_t()
-    assert lib.buzz_paged_workspace_bytes(None, 1, 1, ctypes.byref(n), ctypes.byref(n)) == -1
+    assert lib.buzz_paged_workspace_bytes(None, 1, 1, 0, ctypes.byref(n), ctypes.byref(n)) == -1
     assert lib.buzz_paged_append(None, 0, 256, 256, None, 1, 1, 1, 256, 256, 1, None) == -1
     assert lib.buzz_paged_read(None, 0, 256, 256, None, 1, 1, 1, 256, 256, 1, None) == -1
     assert lib.buzz_paged_decode(None, 0, 256, 256, 256, 1, 1, 1, None, 0, 256, None, 256, 256, None) == -1
