@@ -737,6 +737,71 @@ def test_two_streams_at_once(cuda_device):
     assert all(torch.equal(outs[0][i], out) and torch.equal(outs[1][i], want) for i in range(20))
 
 
+def test_streams_ordered_by_events(cuda_device):
+    """Rows appended on one stream and attended to on another, ordered by events alone, every step a little longer; the
+    steps' results are those of one stream."""
+    g = gen(93)
+    steps, H, d = 40, 4, 64
+    pool, table, _ = make(BF16, E4M3, [steps], 16, 8, H, d, g)
+    t = table.to(DEV)
+    k, v = [torch.randn(steps, H, d, generator=g).to(BF16).to(DEV) for _ in range(2)]
+    q = torch.randn(steps, 1, 8, d, generator=g).to(BF16).to(DEV)
+    lens = [dev_lens([i + 1]) for i in range(steps)]
+    want, got = torch.empty_like(q), torch.empty_like(q)
+    for i in range(steps):
+        pool.append(0, k[i:i + 1], v[i:i + 1], lens[i], t)
+        pool.decode(0, q[i], lens[i], t, steps, want[i])
+    torch.cuda.synchronize()
+    poison(pool)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for i in range(steps):
+        pool.append(0, k[i:i + 1], v[i:i + 1], lens[i], t, stream=a)
+        b.wait_event(a.record_event())
+        pool.decode(0, q[i], lens[i], t, steps, got[i], stream=b)
+        a.wait_event(b.record_event())
+    torch.cuda.synchronize()
+    assert pool.status() == 0 and torch.equal(got, want)
+
+
+def test_paged_and_bounded_steps_in_turn(cuda_device):
+    """Decode steps of bounded caches (which start early behind one another) between steps of a paged one: both as alone."""
+    from tests.harness import make_buzz
+    import workloads
+    w = workloads.scaled(workloads.get("C4"), layers=3, batch=2, q_heads=8, kv_heads=2, prompt_min=300, prompt_max=300, decode_steps=30, window=64, budget=512)
+    outs = []
+    for mixed in (False, True):
+        bz = make_buzz(w)
+        g = gen(94)
+        pool, table, _ = make(BF16, BF16, [40, 40], 32, 8, 2, 128, g)
+        t = table.to(DEV)
+        steps = [workloads.decode_inputs(w, l, DEV) for l in range(3)]
+        for l in range(3):
+            q, k, v, cu = workloads.prefill_inputs(w, l, DEV)
+            bz.prefill(l, q, k, v, cu, 300, torch.empty_like(q))
+        a, p = torch.empty(30, 3, 2, 8, 128, dtype=BF16, device=DEV), torch.empty(30, 3, 2, 8, 128, dtype=BF16, device=DEV)
+        lens = [dev_lens([i + 1] * 2) for i in range(30)]
+
+        def paged(i, l):
+            pool.append(l % 2, steps[l][1][i], steps[l][2][i], lens[i], t)
+            pool.decode(l % 2, steps[l][0][i], lens[i], t, 40, p[i, l])
+
+        torch.cuda.synchronize()
+        for i in range(30):
+            for l in range(3):
+                bz.decode_step(l, steps[l][0][i], steps[l][1][i], steps[l][2][i], a[i, l])
+                if mixed:
+                    paged(i, l)
+        if not mixed:
+            for i in range(30):
+                for l in range(3):
+                    paged(i, l)
+        assert bz.status() == 0 and pool.status() == 0
+        outs.append((a, p))
+        bz.close()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
 def test_paged_and_bounded_caches_side_by_side(cuda_device):
     """While nothing has been evicted, a bounded cache and a paged one of the same layer give the same attention."""
     from tests.harness import make_buzz
