@@ -234,7 +234,7 @@ append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ 
         float x[8];
         unpack(kr[c], x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { lo[c][i] = fminf(lo[c][i], x[i]); hi[c][i] = fmaxf(hi[c][i], x[i]); }
+        for (int i = 0; i < 8; ++i) { lo[c][i] = exact_min(lo[c][i], x[i]); hi[c][i] = exact_max(hi[c][i], x[i]); }
       }
     }
     put_row<T, C, kLanes>(w.k, w.k_scale, base + r, lane, kr, on);
@@ -249,14 +249,14 @@ append_kernel(const PagedView w, const T* __restrict__ k, const T* __restrict__ 
       load8(bnd, p);
       load8(bnd + D, q);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { lo[c][i] = fminf(lo[c][i], p[i]); hi[c][i] = fmaxf(hi[c][i], q[i]); }
+      for (int i = 0; i < 8; ++i) { lo[c][i] = exact_min(lo[c][i], p[i]); hi[c][i] = exact_max(hi[c][i], q[i]); }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
 #pragma unroll
       for (int off = kLanes; off < 32; off <<= 1) {
-        lo[c][i] = fminf(lo[c][i], __shfl_xor_sync(0xffffffffu, lo[c][i], off));
-        hi[c][i] = fmaxf(hi[c][i], __shfl_xor_sync(0xffffffffu, hi[c][i], off));
+        lo[c][i] = exact_min(lo[c][i], __shfl_xor_sync(0xffffffffu, lo[c][i], off));
+        hi[c][i] = exact_max(hi[c][i], __shfl_xor_sync(0xffffffffu, hi[c][i], off));
       }
     }
     if (sub == 0) {

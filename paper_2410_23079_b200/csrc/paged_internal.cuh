@@ -127,6 +127,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// Smaller and larger of two numbers, and one in 64 bits, subnormals included (the build flushes them in fp32
+// arithmetic; bounds of keys are the keys' own values). A NaN gives way to a number.
+__device__ __forceinline__ float exact_min(float x, float y) { float z; asm("min.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y)); return z; }
+__device__ __forceinline__ float exact_max(float x, float y) { float z; asm("max.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y)); return z; }
+__device__ __forceinline__ double exact_double(float x) { double y; asm("cvt.f64.f32 %0, %1;" : "=d"(y) : "f"(x)); return y; }
+
 // Eight consecutive elements of `T` as fp32, and back. The pointer is 16-byte aligned.
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {

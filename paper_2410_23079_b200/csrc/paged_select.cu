@@ -5,11 +5,12 @@
 //   Q+ = sum_h max(q_h, 0), Q- = sum_h min(q_h, 0)
 // so the group's queries collapse into one pair of vectors and a page costs 2 d multiply-adds whatever
 // the group. What is read is 2 d elements per page, which HBM bounds. Sums are fp64: the pages around
-// the border are chosen or left out as a whole, and in fp32 the order of a sum would decide that. The
-// conversions to fp64 (a quarter of the fp32 rate or less) take as long as the traffic, and with the latency
-// of three dependent loads (length, page, bounds) they keep the scores at half of the copy bandwidth: 8
-// sequences of 16384..32768 tokens, 32 KV heads, pages of 32 (98 MB of bounds): 30 us with the pick; one of
-// 131072 tokens, 8 KV heads, pages of 16 (34 MB): 16.7 us.
+// the border are chosen or left out as a whole, and in fp32 the order of a sum would decide that. What keeps
+// the scores at 0.7 of the copy bandwidth is latency: a block is short, and its three dependent loads (length,
+// page, bounds) stand between it and its end. 8 sequences of 16384..32768 tokens, 32 KV heads, pages of 32 (98 MB
+// of bounds): 30 us, 8 of them the pick; one of 131072 tokens, 8 KV heads, pages of 16 (34 MB): 16.7 us, 8 of
+// them the pick. Sums in fp32 take 3 us off either, and were not worth their ties; four heads to a warp, whose
+// bounds lie side by side, take 51 and 28.7 us (four heads' queries to sum before a block can begin).
 //
 // A page belongs to some lanes of a warp, 16 bytes each, and eight pages' loads are under way at once. Scores
 // become unsigned keys that sort like the scores; the top-th largest key is found by histograms, and the
@@ -63,15 +64,21 @@ __device__ __forceinline__ void widen(const uint4& u, float (&x)[16 / sizeof(T)]
   }
 }
 
+// The first of a KV head's queries.
+template <typename T, int D>
+__device__ __forceinline__ const T* queries(const PagedView& w, const SelectArgs& a, int b, int h) {
+  return static_cast<const T*>(a.q) + ((size_t)b * w.kv_heads + h) * a.group * D;
+}
+
 // The group's queries by sign, summed, for the smallest values and then the largest: qsum[2 * D], by all threads.
 template <typename T, int D, int kThreads>
-__device__ __forceinline__ void sum_queries(const SelectArgs& a, int kv_heads, int b, int h, double* qsum) {
+__device__ __forceinline__ void sum_queries(const PagedView& w, const SelectArgs& a, int b, int h, double* qsum) {
   for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
-    const T* q = static_cast<const T*>(a.q) + ((size_t)b * kv_heads + h) * a.group * D + i % D;
+    const T* q = queries<T, D>(w, a, b, h) + i % D;
     double sum = 0.0;
     for (int g = 0; g < a.group; ++g) {
-      const float x = (float)q[g * D];
-      sum += (double)((x < 0.f) == (i < D) || x != x ? x : 0.f);
+      const double x = exact_double((float)q[g * D]);
+      sum += (x < 0.0) == (i < D) || x != x ? x : 0.0;
     }
     qsum[i] = sum;
   }
@@ -86,11 +93,29 @@ __device__ __forceinline__ int look_up(const PagedView& w, const SelectArgs& a, 
   return -1;
 }
 
+// A page's score term by term, by the whole warp: for pages whose score by sums is not finite. A half of the sums that is
+// zero makes NaN of an infinite bound that no query reaches, and where all keys were NaN the bounds are crossed.
+template <typename T, int D>
+__device__ __noinline__ double score_by_terms(const PagedView w, const T* q, int group, int h, int page) {
+  const T* lo = reinterpret_cast<const T*>(w.bounds) + ((size_t)page * w.kv_heads + h) * 2 * D;
+  double s = 0.0;
+  for (int i = threadIdx.x & 31; i < D; i += 32) {
+    const double l = exact_double((float)lo[i]), u = exact_double((float)lo[D + i]);
+    for (int g = 0; g < group; ++g) {
+      const double x = exact_double((float)q[g * D + i]), low = x * l, high = x * u;
+      s += low != low || low > high ? low : high;           // NaN if either is
+    }
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+  return s;
+}
+
 // Keys of the kOfWarp pages from lp0 on (those below `end`), by one warp; `mine` is the physical page of the lane's page,
-// number wl % kLanes of the lane group's.
-// `put(i, key)` takes the key of logical page i.
+// number wl % kLanes of the lane group's, `q` the group's first query. `put(i, key)` takes the key of logical page i.
 template <typename T, int D, typename Put>
-__device__ __forceinline__ void score_pages(const PagedView& w, int h, int lp0, int end, int mine, const double* qsum, Put&& put) {
+__device__ __forceinline__ void score_pages(const PagedView& w, const T* q, int group, int h, int lp0, int end, int mine, const double* qsum,
+                                            Put&& put) {
   using L = ScorePlan<T, D>;
   constexpr int kE = L::kE, kLanes = L::kLanes, kCL = L::kCL;
   const int wl = threadIdx.x & 31, lane = wl % kLanes, sub = wl / kLanes;
@@ -122,7 +147,7 @@ __device__ __forceinline__ void score_pages(const PagedView& w, int h, int lp0, 
         float x[kE];
         widen<T>(raw[i][c], x);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) s[i] += qs[e] * (double)x[e];
+        for (int e = 0; e < kE; ++e) s[i] += qs[e] * exact_double(x[e]);
       }
     }
     if (batch + 1 < L::kBatches) fetch(batch + 1);
@@ -143,6 +168,12 @@ __device__ __forceinline__ void score_pages(const PagedView& w, int h, int lp0, 
     constexpr int kRest = kLanes / kBatch;                  // lanes that now hold one page's sum
     const int i = batch * kBatch + lane / kRest;
     const int page = __shfl_sync(0xffffffffu, mine, i, kLanes);
+    const bool odd = lane % kRest == 0 && page >= 0 && !(fabs(s[0]) <= 1.7e308);
+    for (unsigned left = __ballot_sync(0xffffffffu, odd); left != 0; left &= left - 1) {
+      const int of = __ffs(left) - 1;
+      const double by_terms = score_by_terms<T, D>(w, q, group, h, __shfl_sync(0xffffffffu, page, of));
+      if (wl == of) s[0] = by_terms;
+    }
     if (lane % kRest == 0 && p0 + i < end) put(p0 + i, page >= 0 ? ordered_key(s[0]) : 0ull);      // a bad page is below all others
   }
 }
@@ -171,11 +202,11 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView
   __shared__ double qsum[2 * D];
   const int lp0 = block0 + threadIdx.x / 32 * kOfWarp;
   const int mine = look_up_mine<T, D>(w, a, b, lp0, end);
-  sum_queries<T, D, kScoreWarps * 32>(a, w.kv_heads, b, h, qsum);
+  sum_queries<T, D, kScoreWarps * 32>(w, a, b, h, qsum);
   __syncthreads();
   if (lp0 >= end) return;
   unsigned long long* keys = a.keys + ((size_t)b * w.kv_heads + h) * a.max_pages;
-  score_pages<T, D>(w, h, lp0, end, mine, qsum, [&](int i, unsigned long long key) { keys[i] = key; });
+  score_pages<T, D>(w, queries<T, D>(w, a, b, h), a.group, h, lp0, end, mine, qsum, [&](int i, unsigned long long key) { keys[i] = key; });
 }
 
 // The pick, by one block. A histogram of kBins equal bins over the keys' range finds the bin that holds the
@@ -396,11 +427,12 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const PagedView 
   constexpr int kSweep = kSelectThreads / 32 * ScorePlan<T, D>::kOfWarp;
   int lp0 = a.sink + threadIdx.x / 32 * ScorePlan<T, D>::kOfWarp;
   int mine = look_up_mine<T, D>(w, a, b, lp0, end);
-  sum_queries<T, D, kSelectThreads>(a, w.kv_heads, b, h, qsum);
+  sum_queries<T, D, kSelectThreads>(w, a, b, h, qsum);
   __syncthreads();
   for (; lp0 < end; lp0 += kSweep) {
     const int then = look_up_mine<T, D>(w, a, b, lp0 + kSweep, end);  // under way while these pages are scored
-    score_pages<T, D>(w, h, lp0, end, mine, qsum, [&](int i, unsigned long long key) { select_keys[i - a.sink] = key; });
+    score_pages<T, D>(w, queries<T, D>(w, a, b, h), a.group, h, lp0, end, mine, qsum,
+                      [&](int i, unsigned long long key) { select_keys[i - a.sink] = key; });
     mine = then;
   }
   __syncthreads();

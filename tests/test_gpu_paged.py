@@ -493,13 +493,50 @@ def test_select_special_scores(cuda_device):
     pool.bounds[0, table[0, :10].long()] = b.to(DEV)
     q = torch.zeros(1, 1, 64)
     q[0, 0, 0] = 1.0
-    b[3, 0, :, 1:] = 0.0
     for top in range(0, 9):
         sel = torch.empty(1, 1, top + 1, dtype=torch.int32, device=DEV)
         pool.select(0, q.to(DEV), dev_lens([160]), table.to(DEV), 160, 0, 1, top, sel)
-        # NaN: 6 (a NaN bound); 3 and 4 (infinity times the zeros of the other sign's half is NaN as well)
-        order = [3, 4, 6, 7, 0, 1, 5, 8, 2]
+        order = [6, 3, 7, 0, 1, 5, 8, 2, 4]                   # NaN (a NaN bound), infinity, 2, zeros, -1, -infinity
         assert sel[0, 0].tolist() == sorted(order[:top]) + [9], top
+
+
+@pytest.mark.parametrize("dtype,d,H,group", [(BF16, 128, 2, 4), (BF16, 64, 1, 1), (F32, 64, 3, 2), (F32, 128, 1, 8)])
+@pytest.mark.parametrize("pages", [60, 700])
+def test_select_with_infinite_and_nan_keys(cuda_device, dtype, d, H, group, pages):
+    """Keys that hold infinities and NaN, whole pages of NaN, and queries that do and do not reach them."""
+    g = gen(pages + d)
+    pool, table, _ = make(dtype, dtype, [16 * pages], 16, H * group, H, d, g)
+    k = torch.randn(pages, 16, H, d, generator=g).to(dtype)
+    for i in range(0, pages, 3):
+        k[i, int(torch.randint(16, (1,), generator=g)), :, int(torch.randint(d, (1,), generator=g))] = (math.inf, -math.inf, math.nan)[i // 3 % 3]
+    k[7, :, :, 3], k[8] = math.nan, math.nan
+    k = k.view(-1, H, d)
+    pool.append(0, k.to(DEV), k.to(DEV), dev_lens([16 * pages]), table.to(DEV), cu_of([16 * pages]).to(DEV))
+    bounds = ref.page_bounds(k, 16)
+    q = torch.randn(1, H * group, d, generator=g)
+    for q in (q, q.abs(), -q.abs(), q * (torch.rand(1, H * group, d, generator=g) < 0.5)):
+        q = q.to(dtype)
+        for top in (1, 4, 15, 40):
+            sel = torch.empty(1, H, top + 2, dtype=torch.int32, device=DEV)
+            pool.select(0, q.to(DEV), dev_lens([16 * pages]), table.to(DEV), 16 * pages, 1, 1, top, sel)
+            assert sel[0].tolist() == ref.choose(q[0], bounds, 1, 1, top), top
+    assert pool.status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_bounds_and_scores_of_subnormal_keys(cuda_device, dtype):
+    g = gen(77)
+    pool, table, _ = make(dtype, dtype, [1600], 16, 2, 1, 64, g)
+    k = (torch.randn(1600, 1, 64, generator=g).double() * 2.0 ** -130).to(dtype)
+    pool.append(0, k.to(DEV), k.to(DEV), dev_lens([1600]), table.to(DEV), cu_of([1600]).to(DEV))
+    bounds = ref.page_bounds(k, 16)
+    assert float(bounds.abs().max()) > 0
+    assert torch.equal(pool.bounds[0, table[0, :100].long()].double().cpu(), bounds)
+    for scale in (1.0, 2.0 ** -130):
+        q = (torch.randn(1, 2, 64, generator=g).double() * scale).to(dtype)
+        sel = torch.empty(1, 1, 12, dtype=torch.int32, device=DEV)
+        pool.select(0, q.to(DEV), dev_lens([1600]), table.to(DEV), 1600, 1, 1, 10, sel)
+        assert sel[0].tolist() == ref.choose(q[0], bounds, 1, 1, 10)
 
 
 def test_select_bad_lengths_and_pages(cuda_device):
