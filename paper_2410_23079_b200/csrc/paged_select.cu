@@ -6,11 +6,12 @@
 // so the group's queries collapse into one pair of vectors and a page costs 2 d multiply-adds whatever
 // the group. What is read is 2 d elements per page, which HBM bounds. Sums are fp64: the pages around
 // the border are chosen or left out as a whole, and in fp32 the order of a sum would decide that. What keeps
-// the scores at 0.7 of the copy bandwidth is latency: a block is short, and its three dependent loads (length,
+// the scores at 0.65 of the copy bandwidth is latency: a block is short, and its three dependent loads (length,
 // page, bounds) stand between it and its end. 8 sequences of 16384..32768 tokens, 32 KV heads, pages of 32 (98 MB
-// of bounds): 30 us, 8 of them the pick; one of 131072 tokens, 8 KV heads, pages of 16 (34 MB): 16.7 us, 8 of
-// them the pick. Sums in fp32 take 3 us off either, and were not worth their ties; four heads to a warp, whose
-// bounds lie side by side, take 51 and 28.7 us (four heads' queries to sum before a block can begin).
+// of bounds): 29 us, with the pick's launch and its 3 us; one of 131072 tokens, 8 KV heads, pages of 16 (34 MB):
+// 15.3 us, with the pick's launch and its 4 us. Sums in fp32 would take 2 us off, and were not worth their ties;
+// four heads to a warp, whose bounds lie side by side, take 51 and 28.7 us (four heads' queries to sum first).
+// Infinite bounds are rare and answered apart, so that a page's score is the formula's whatever its keys are.
 //
 // A page belongs to some lanes of a warp, 16 bytes each, and eight pages' loads are under way at once. Scores
 // become unsigned keys that sort like the scores; the top-th largest key is found by histograms, and the
@@ -212,12 +213,14 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const PagedView
 // The pick, by one block. A histogram of kBins equal bins over the keys' range finds the bin that holds the
 // border; its keys (a handful where the scores spread) are ranked against one another, and the one of the
 // wanted rank is the last that is kept. A crowded bin is cut into kBins once more, down to single values;
-// pages of one value are ranked by their number.
-constexpr int kBins = 2048;
+// pages of one value are ranked by their number. A thread has two bins: more of them are slower to look
+// through than the border's bin gets smaller (eight: 0.3 us of 6.7 for 125 pages, 0.8 of 30 for 256 picks).
 constexpr int kRanked = 256;         // keys that are ranked directly
 
 template <int kThreads>
 struct PickSpace {
+  static constexpr int kLog = kThreads == 1024 ? 11 : 9, kBins = 1 << kLog;
+  static_assert(kBins == 2 * kThreads, "two bins a thread");
   int hist[kBins];
   unsigned long long cand[kRanked], last_key;
   uint32_t ends[2][kThreads / 32];
@@ -250,7 +253,7 @@ __device__ __forceinline__ int pick_ends(const PagedView& w, const SelectArgs& a
 template <int kThreads, int kHeld>
 __device__ __forceinline__ void pick_largest(const unsigned long long* keys, int n, int top, int first, int32_t* out, PickSpace<kThreads>& sp) {
   typedef unsigned long long u64;
-  constexpr int kWarps = kThreads / 32, kOwn = kBins / kThreads;       // bins of a thread
+  constexpr int kWarps = kThreads / 32, kLog = PickSpace<kThreads>::kLog, kBins = 1 << kLog, kOwn = kBins / kThreads;       // bins of a thread
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
   // key i of the thread is that of page i * kThreads + tid; the first kHeld are kept in registers
   u64 held[kHeld > 0 ? kHeld : 1];
@@ -309,7 +312,7 @@ __device__ __forceinline__ void pick_largest(const unsigned long long* keys, int
   {
     uint32_t low = small, reach = large - small;
     for (;;) {
-      const int shift = max(0, 32 - __clz((int)reach) - 11);
+      const int shift = max(0, 32 - __clz((int)reach) - kLog);
       each([&](u64 k, int) {
         const uint32_t u = (uint32_t)(k >> 32) - low;
         if (u <= reach) atomicAdd(&sp.hist[u >> shift], 1);
@@ -324,7 +327,7 @@ __device__ __forceinline__ void pick_largest(const unsigned long long* keys, int
     span = ((u64)reach << 32) | 0xffffffffu;
   }
   while (sp.border_count > kRanked && span > 0) {  // one upper half so far
-    const int shift = max(0, 64 - __clzll((long long)span) - 11);
+    const int shift = max(0, 64 - __clzll((long long)span) - kLog);
     each([&](u64 k, int) { if (k - base <= span) atomicAdd(&sp.hist[(int)((k - base) >> shift)], 1); });
     find_border(rest);
     base += (u64)sp.border << shift;
