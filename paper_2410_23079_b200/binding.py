@@ -322,7 +322,7 @@ def _token_stride(name, x, device, dtype, tokens, heads, d):
     """Elements between the tokens of [tokens, heads, d], whose heads are contiguous."""
     s0, s1, s2 = x.stride()
     if x.device == device and x.dtype is dtype and x.shape == (tokens, heads, d) and s2 == 1 and (s1 == d or heads == 1):
-        return s0 if tokens > 1 else max(s0, heads * d)
+        return s0 if tokens > 1 else heads * d
     _need(x.device == device, f"{name}: on {x.device}, not on {device}")
     _need(x.dtype is dtype, f"{name}: {x.dtype}, not {dtype}")
     _need(x.shape == (tokens, heads, d), f"{name}: shape {tuple(x.shape)}, not {(tokens, heads, d)}")
@@ -386,8 +386,9 @@ def norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps=1e
         raise ValueError(f"q: on {device}; there is no CPU fallback")
     if dtype not in _DTYPES:
         raise ValueError(f"q: {dtype} is not supported")
-    if (q.requires_grad or k.requires_grad) and torch.is_grad_enabled():
-        raise ValueError("q and k: the rotation has no backward pass; detach them or call under torch.no_grad()")
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or q_weight is not None and q_weight.requires_grad
+                                    or k_weight is not None and k_weight.requires_grad):
+        raise ValueError("q, k and weights: the rotation has no backward pass; detach them or call under torch.no_grad()")
     T, Hq, d = q.shape
     Hk = k.shape[1]
     pos, freq = _tensor("positions", positions, device, torch.int32, (T,)), _tensor("inv_freq", inv_freq, device, torch.float32, (None,))
@@ -517,6 +518,7 @@ class BuzzPaged:
         ep = None if lse is None else _tensor("lse", lse, self.device, torch.float32, (batch, self.q_heads))
         sp = None if selected is None else _tensor("selected", selected, self.device, torch.int32, (batch, self.kv_heads, None))
         stride = 0 if selected is None else selected.shape[2]
+        _need(selected is None or stride > 0, "selected: names no page")
         with _on(self.device, stream) as s:
             ws, n = self._workspace(batch, max_len, stride, False)
             rc = self._lib.buzz_paged_decode(self._h, layer, qp, lp, tp, width, batch, max_len, sp, stride, op, ep,

@@ -217,6 +217,7 @@ extern "C" int buzz_norm_rope(const buzz_rope_shape* sh, const void* q, const vo
   if (sh->q_stride < qrow || sh->q_out_stride < qrow || sh->k_stride < krow || sh->k_out_stride < krow) return BUZZ_ERR_INVALID;
   if ((sh->q_stride | sh->q_out_stride | sh->k_stride | sh->k_out_stride) % unit) return BUZZ_ERR_INVALID;
   if (tokens == 0) return BUZZ_OK;
+  if (tokens > 1 && ((q_out == q && sh->q_out_stride != sh->q_stride) || (k_out == k && sh->k_out_stride != sh->k_stride))) return BUZZ_ERR_INVALID;
   if (!q || !k || !positions_dev || !inv_freq_dev || !q_out || !k_out) return BUZZ_ERR_INVALID;
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_weight) || !aligned16(k_weight) ||
       (reinterpret_cast<uintptr_t>(positions_dev) | reinterpret_cast<uintptr_t>(inv_freq_dev)) & 3u)

@@ -82,6 +82,22 @@ def test_norm_rope_refusals(cuda_device):
             norm_rope(q, q, p, bad)
     with pytest.raises(BuzzError):
         norm_rope(q, q, p, f, eps=-1.0)
+    w = torch.ones(64, device=DEV, requires_grad=True)
+    with pytest.raises(ValueError):
+        norm_rope(q, q, p, f, q_weight=w)
+    with pytest.raises(ValueError):
+        norm_rope(q, q, p, f, k_weight=w)
+    with torch.no_grad():
+        norm_rope(q, q, p, f, q_weight=w)
+
+
+def test_norm_rope_of_one_token_whatever_its_stride(cuda_device):
+    """A single token's rows have no distance that could be wrong."""
+    x = torch.randn(3, 5, 64, generator=gen(9)).to(BF16).to(DEV)
+    one = x.as_strided((1, 4, 64), (259, 64, 1))
+    p, f = torch.tensor([77], dtype=torch.int32, device=DEV), torch.ones(16, device=DEV)
+    got, want = norm_rope(one, one, p, f), norm_rope(x[:1, :4], x[:1, :4], p, f)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 # ---- pool helpers --------------------------------------------------------------------------------
@@ -640,6 +656,7 @@ def test_refusals(cuda_device):
                  lambda: pool.decode(0, q, lens.long(), t, 40, out), lambda: pool.decode(0, q, lens, t[:1], 40, out),
                  lambda: pool.decode(0, q, lens, t.cpu(), 40, out), lambda: pool.decode(0, q, lens, t, 40, out.transpose(0, 1)),
                  lambda: pool.decode(0, q, lens, t, 40, out, lse=out[..., 0]), lambda: pool.decode(0, q, lens, t, 40, out, selected=sel[:, :1]),
+                 lambda: pool.decode(0, q, lens, t, 40, out, selected=sel[..., :0].contiguous()),
                  lambda: pool.append(0, x, x[:1], lens, t), lambda: pool.append(0, x[:1], x[:1], lens, t),
                  lambda: pool.append(0, x.float(), x.float(), lens, t), lambda: pool.append(0, x, x, lens, t, cu_seqlens=lens),
                  lambda: pool.select(0, q, lens, t, 40, 1, 1, 2, sel), lambda: pool.select(0, q, lens, t, 40, 0, 1, 2, sel.float())):

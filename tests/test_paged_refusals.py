@@ -32,6 +32,8 @@ def test_norm_rope_pointers():
         assert lib.buzz_norm_rope(ctypes.byref(sh), *args, 4, None) == -1, (i, bad)
     assert lib.buzz_norm_rope(ctypes.byref(sh), *good, -1, None) == -1
     assert lib.buzz_norm_rope(None, *good, 4, None) == -1
+    for over in (dict(q_out_stride=2048), dict(k_out_stride=512)):                    # in place, but not where the rows were
+        assert lib.buzz_norm_rope(ctypes.byref(binding._RopeShape(**{**OK_ROPE, **over})), 256, 512, 256, 256, None, None, 256, 512, 4, None) == -1
     assert lib.buzz_norm_rope(ctypes.byref(sh), *[None] * 8, 0, None) == 0          # no tokens: nothing to do
 
 
